@@ -262,6 +262,81 @@ sod2_status sod2_run_output_shape(sod2_plan_t* p, const void* arena, void* cuda_
 sod2_status sod2_nonzero_static(const void* dev_x, int dtype, int rank, const int64_t* dims, int64_t* dev_out,
                                 int64_t* dev_count, void* cuda_stream);
 
+/* ---- operators of a serving loop, as direct calls ----
+ * For programs that keep their own loop around a network (token by token, a batch whose lengths change with every step) and
+ * own all device memory.  The paper has no counterpart; the packing is that of its dynamic batches: the rows of all requests
+ * back to back, no padding to a maximum length.  ALL LENGTHS LIVE ON THE DEVICE, so that a captured CUDA graph of these calls
+ * replays with other lengths; the host gives upper bounds.  Every call is asynchronous on cuda_stream, allocates nothing, keeps
+ * nothing between calls and has the same results for the same inputs.  The device that holds the tensors must be the current
+ * device and own cuda_stream.  Outputs must not overlap inputs unless a call says so.  Whatever the lengths, tables and slots hold,
+ * nothing outside the described tensors is read or written.
+ *
+ * dev_status (device, may be NULL) collects bits that calls set and never clear:
+ *   1  a bounded wait in a kernel ran out: the results of the call are not valid
+ *   2  a page id or a slot outside the cache was met: it was not followed (keys and values of such a page count as zeros, rows
+ *      with such a slot are not stored); a negative slot is no error, it means "do not store"
+ *   4  the free list or the width of the table ran out: the tokens without a page have slot -1
+ *   8  a negative length (taken as 0), or more new tokens than max_tokens (the rows behind it are left out)
+ * Errors of all calls: SOD2_E_INVALID_ARG, SOD2_E_BAD_DIM, SOD2_E_MISALIGNED, SOD2_E_ARENA_TOO_SMALL (workspace), SOD2_E_CUDA;
+ * message through sod2_last_error(NULL). */
+#define SOD2_DTYPE_F32 0
+#define SOD2_DTYPE_BF16 1
+#define SOD2_DTYPE_F16 4
+/* [tokens, heads, head_dim]: strides in elements, the head_dim elements of a row consecutive */
+typedef struct { void* data; int64_t token_stride, head_stride; } sod2_rows;
+/* [pages, page_size, heads, head_dim] in any order of the first three extents */
+typedef struct { void* data; int64_t page_stride, token_stride, head_stride; } sod2_pages;
+
+/* Block tables and slot map of one step, from the requests' lengths.  Request r has dev_past[r] tokens in the cache and dev_new[r]
+ * new ones.  The pages it lacks, ceil((past + new) / page_size) - ceil(past / page_size), are taken from dev_free_pages[n_free],
+ * request after request, from entry *dev_free_head (NULL: 0) on, and written to its row of dev_table behind those it has (the
+ * rest of the row is left as it was); *dev_free_head_out = the first entry not taken.
+ *   dev_cu_tokens[n_requests + 1]  first packed row of each request (clamped to max_tokens);  dev_ctx[n_requests] = past + new
+ *   dev_slots[max_tokens]          id * page_size + offset of each new token, -1 in the rows behind the last request
+ *   dev_positions[max_tokens]      (may be NULL) position of each new token in its request, -1 behind the last
+ * dev_ctx must not be dev_past or dev_new, nor dev_free_head_out dev_free_head: these are refused. */
+sod2_status sod2_page_tables(int n_requests, int64_t max_tokens, int page_size, const int32_t* dev_past, const int32_t* dev_new,
+                             const int32_t* dev_free_pages, int64_t n_free, const int32_t* dev_free_head, int32_t* dev_table,
+                             int64_t table_stride, int64_t table_width, int32_t* dev_cu_tokens, int32_t* dev_ctx, int64_t* dev_slots,
+                             int32_t* dev_positions, int32_t* dev_free_head_out, int32_t* dev_status, void* cuda_stream);
+
+/* Rotary positions with any number of axes (text, images, video) and, where caches are given, the store of keys and values.
+ * Pair j of every head is turned by freq[j] * dev_positions[axis[j] * axis_stride + token] radians (freq and axis: host arrays of
+ * n_pairs): (x, y) -> (x cos - y sin, y cos + x sin).  The pair is (j, j + n_pairs), or with adjacent = 1 (2j, 2j + 1);
+ * elements from 2 n_pairs on pass unchanged.  Angles are reduced in 64 bits.
+ * q -> q_out (both NULL with n_heads = 0) and k -> k_out (may be the same rows: in place) for all n_tokens rows; with k_cache /
+ * v_cache, the turned key and the value of row t go to slot dev_slots[t] (page slot / page_size, offset slot % page_size)
+ * unless it is negative.  Two rows with the same slot: either may be the one that stays.  dtype: f32, bf16, f16. */
+sod2_status sod2_rope_store(int dtype, int64_t n_tokens, int n_heads, int n_kv_heads, int head_dim, int n_pairs, const double* freq,
+                            const uint8_t* axis, int adjacent, const int32_t* dev_positions, int64_t axis_stride, const sod2_rows* q,
+                            const sod2_rows* q_out, const sod2_rows* k, const sod2_rows* k_out, const sod2_rows* v,
+                            const sod2_pages* k_cache, const sod2_pages* v_cache, int64_t n_pages, int page_size,
+                            const int64_t* dev_slots, int32_t* dev_status, void* cuda_stream);
+
+/* Bytes of device workspace (256-byte aligned) for the two attention calls with these heads, whatever the number and lengths of
+ * requests.  Calls that may overlap on the GPU need a workspace each; two captured graphs that never overlap may share one. */
+sod2_status sod2_attention_workspace_bytes(int n_heads, int n_kv_heads, int head_dim, size_t* bytes);
+
+/* Causal attention over packed prompts with grouped heads: request r has the rows dev_cu_tokens[r] .. dev_cu_tokens[r + 1] - 1 of q,
+ * k, v and out; row i of a request attends to its rows 0 .. i; query head h to key head h / (n_heads / n_kv_heads).
+ * out_i = sum_j softmax_j(scale * q_i . k_j) v_j.  Rows of out outside the requests are left as they were.  dtype: f32, bf16, f16;
+ * head_dim 1..256. */
+sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t n_tokens, int n_heads, int n_kv_heads, int head_dim,
+                                  const sod2_rows* q, const sod2_rows* k, const sod2_rows* v, const sod2_rows* out,
+                                  const int32_t* dev_cu_tokens, float scale, void* dev_workspace, size_t workspace_bytes,
+                                  int32_t* dev_status, void* cuda_stream);
+
+/* Attention of new tokens (one, or a chunk) over a paged cache that already holds their keys and values: request r has n =
+ * dev_cu_tokens[r + 1] - dev_cu_tokens[r] query rows and dev_ctx[r] keys in the pages dev_table[r * table_stride ..]; its row i attends to
+ * the keys 0 .. ctx - n + i (a row for which that is none becomes zero).  ctx beyond table_width * page_size counts as
+ * that.  What the cache holds behind the last key does not matter, whatever it is.  max_new: the host's bound on n (0: unknown),
+ * used to choose a kernel, never for the result.  Rows of out outside the requests are left as they were. */
+sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n_tokens, int64_t max_new, int n_heads, int n_kv_heads,
+                                 int head_dim, const sod2_rows* q, const sod2_rows* out, const int32_t* dev_cu_tokens,
+                                 const int32_t* dev_ctx, const sod2_pages* k_cache, const sod2_pages* v_cache, int64_t n_pages,
+                                 int page_size, const int32_t* dev_table, int64_t table_stride, int64_t table_width, float scale,
+                                 void* dev_workspace, size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
+
 /* Launches one kernel that does nothing (one thread, no arguments) on cuda_stream.  A measuring aid:
  * the smallest fused groups (a few thousand elements per request) take about as long as this launch,
  * so their time is reported as a multiple of it rather than as a fraction of a roofline.

@@ -84,6 +84,11 @@ def _load() -> C.CDLL:
         "sod2_plan_tensor_strides": [vp, cp, i32, P(i64), P(i32)],
         "sod2_run_output_shape": [vp, vp, vp, i32, i32, P(i64), P(i32)],
         "sod2_nonzero_static": [vp, i32, i32, P(i64), vp, vp, vp],
+        "sod2_page_tables": [i32, i64, i32, vp, vp, vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp],
+        "sod2_rope_store": [i32, i64, i32, i32, i32, i32, vp, vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, i32, vp, vp, vp],
+        "sod2_attention_workspace_bytes": [i32, i32, i32, P(sz)],
+        "sod2_attention_prompt": [i32, i32, i64, i32, i32, i32, vp, vp, vp, vp, vp, C.c_float, vp, sz, vp, vp],
+        "sod2_attention_paged": [i32, i32, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, i32, vp, i64, i64, C.c_float, vp, sz, vp, vp],
         "sod2_launch_empty": [vp],
         "sod2_selftest_bounded_wait": [vp, vp],
         "sod2_selftest_mma_rate": [i32, i32, i32, i32, i32, i32, vp, P(C.c_double)],
@@ -111,7 +116,8 @@ EXPORTS = ["sod2_graph_create", "sod2_graph_destroy", "sod2_graph_set_const", "s
            "sod2_graph_num_ops", "sod2_graph_op_info", "sod2_graph_num_groups", "sod2_graph_group_info",
            "sod2_graph_num_subgraphs", "sod2_graph_rdp_sweeps", "sod2_classify", "sod2_graph_reanalyse", "sod2_graph_order_info",
            "sod2_binding_shape", "sod2_plan_slot", "sod2_plan_instance_offset", "sod2_plan_memory", "sod2_plan_group_cost", "sod2_plan_group_on_side_stream", "sod2_plan_io_counts", "sod2_plan_group_form", "sod2_plan_tensor_strides",
-           "sod2_run_output_shape", "sod2_nonzero_static", "sod2_launch_empty", "sod2_selftest_bounded_wait", "sod2_selftest_mma_rate", "sod2_last_error"]
+           "sod2_run_output_shape", "sod2_nonzero_static", "sod2_page_tables", "sod2_rope_store", "sod2_attention_workspace_bytes", "sod2_attention_prompt", "sod2_attention_paged",
+           "sod2_launch_empty", "sod2_selftest_bounded_wait", "sod2_selftest_mma_rate", "sod2_last_error"]
 
 
 def _check(status: int, handle=None):
@@ -155,6 +161,82 @@ def sod2_nonzero_static(dev_x: int, dtype: int, dims: Sequence[int], dev_out: in
     d = (C.c_int64 * max(len(dims), 1))(*[int(v) for v in dims])
     _check(lib.sod2_nonzero_static(C.c_void_p(dev_x), dtype, len(dims), d, C.c_void_p(dev_out), C.c_void_p(dev_count),
                                    C.c_void_p(stream)))
+
+
+# ---- operators of a serving loop.  Addresses are integers (a tensor's data_ptr()); rows are (address, token stride, head stride),
+# caches (address, page stride, token stride, head stride), strides in elements.  See include/sod2.h.
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 4
+
+
+class Rotation:
+    """Frequencies (radians per position) and axes of the rotated pairs of a head; adjacent: pairs (2j, 2j + 1) instead of
+    (j, j + n).  Kept by the program, handed to every sod2_rope_store."""
+
+    def __init__(self, freq: Sequence[float], axis: Sequence[int], adjacent: bool = False):
+        if len(freq) != len(axis) or not freq:
+            raise ValueError("a frequency and an axis per rotated pair are wanted")
+        if any(a < 0 or a > 255 for a in axis):
+            raise ValueError("axes must be 0..255")
+        self.n_pairs, self.adjacent = len(freq), int(bool(adjacent))
+        self._freq, self._axis = (C.c_double * len(freq))(*freq), (C.c_uint8 * len(axis))(*axis)
+        self.freq, self.axis = C.addressof(self._freq), C.addressof(self._axis)
+
+    @classmethod
+    def sections(cls, sections: Sequence[int], theta: float = 10000.0, local: bool = False, adjacent: bool = False) -> "Rotation":
+        """sections[a] pairs turn with axis a.  local: every axis has the whole ladder of frequencies in its section (images,
+        video), else one ladder theta^(-j / n) runs over all sections."""
+        total = sum(sections)
+        freq, axis = [], []
+        for a, n in enumerate(sections):
+            for j in range(n):
+                freq.append(theta ** -(j / n if local else len(freq) / total))
+                axis.append(a)
+        return cls(freq, axis, adjacent)
+
+
+def sod2_page_tables(n_requests: int, max_tokens: int, page_size: int, past: int, new: int, free_pages: int, n_free: int, free_head: Optional[int],
+                     table: int, table_stride: int, table_width: int, cu_tokens: int, ctx: int, slots: int, positions: Optional[int],
+                     free_head_out: int, status: Optional[int], stream: int) -> None:
+    """Block tables and slot map of one step, built on the GPU from the requests' lengths."""
+    st = _calls.page_tables(n_requests, max_tokens, page_size, past, new, free_pages, n_free, free_head, table, table_stride, table_width, cu_tokens, ctx,
+                            slots, positions, free_head_out, status, stream)
+    if st:
+        _check(st)
+
+
+def sod2_rope_store(dtype: int, n_tokens: int, n_heads: int, n_kv_heads: int, head_dim: int, rotation: Rotation, positions: int, axis_stride: int,
+                    q, q_out, k, k_out, v, k_cache, v_cache, n_pages: int, page_size: int, slots: Optional[int], status: Optional[int],
+                    stream: int) -> None:
+    """Rotary positions of queries and keys; with caches, the store of keys and values at their slots.  Absent tensors: None."""
+    st = _calls.rope_store(dtype, n_tokens, n_heads, n_kv_heads, head_dim, rotation.n_pairs, rotation.freq, rotation.axis, rotation.adjacent,
+                           positions, axis_stride, q, q_out, k, k_out, v, k_cache, v_cache, n_pages, page_size, slots, status, stream)
+    if st:
+        _check(st)
+
+
+def sod2_attention_workspace_bytes(n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    n = C.c_size_t()
+    _check(lib.sod2_attention_workspace_bytes(n_heads, n_kv_heads, head_dim, C.byref(n)))
+    return n.value
+
+
+def sod2_attention_prompt(dtype: int, n_requests: int, n_tokens: int, n_heads: int, n_kv_heads: int, head_dim: int, q, k, v, out, cu_tokens: int,
+                          scale: float, workspace: int, workspace_bytes: int, status: Optional[int], stream: int) -> None:
+    """Causal attention over packed prompts with grouped heads."""
+    st = _calls.attention_prompt(dtype, n_requests, n_tokens, n_heads, n_kv_heads, head_dim, q, k, v, out, cu_tokens, scale, workspace, workspace_bytes,
+                                 status, stream)
+    if st:
+        _check(st)
+
+
+def sod2_attention_paged(dtype: int, n_requests: int, n_tokens: int, max_new: int, n_heads: int, n_kv_heads: int, head_dim: int, q, out, cu_tokens: int,
+                         ctx: int, k_cache, v_cache, n_pages: int, page_size: int, table: int, table_stride: int, table_width: int, scale: float,
+                         workspace: int, workspace_bytes: int, status: Optional[int], stream: int) -> None:
+    """Attention of new tokens, one or a chunk per request, over a paged cache that holds their keys and values."""
+    st = _calls.attention_paged(dtype, n_requests, n_tokens, max_new, n_heads, n_kv_heads, head_dim, q, out, cu_tokens, ctx, k_cache, v_cache, n_pages,
+                                page_size, table, table_stride, table_width, scale, workspace, workspace_bytes, status, stream)
+    if st:
+        _check(st)
 
 
 class Graph:

@@ -1,0 +1,102 @@
+// Causal attention with grouped heads over packed requests, keys and values either packed beside the queries or in a paged cache:
+//   o_i = sum_j softmax_j(scale q_i . k_j) v_j   over the keys j <= ctx - n + i of the request,
+// n new tokens of the request, ctx of its tokens with keys (a prompt: n = ctx).  Rows without a key are zero.
+// This kernel takes every type, head size up to 256, stride, alignment and page size; attention_causal_tcgen05.cuh takes what
+// tensor maps can express.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "kernels_paging.cuh"
+
+namespace sod2 {
+namespace k {
+
+struct CausalParams {
+  const void* q; const void* k; const void* v; void* o;
+  long long q_ts, q_hs, o_ts, o_hs;
+  long long k_ps, k_ts, k_hs, v_ps, v_ts, v_hs;    // page (0 without a cache), token and head strides in elements
+  const int* cu;                                   // [n_req + 1] first rows
+  const int* ctx;                                  // [n_req], null: prompts, the keys are rows of k and v
+  const int* table; long long table_stride;        // [n_req][width] page ids
+  int* status;
+  int n_req, n_tokens, H, HK, D, page, width, n_pages;
+  float scale;
+};
+
+// The request of a packed row, and where the row stands in it.  Lengths are taken as they are on the device: whatever they
+// hold, rows stay below n_tokens and keys within the table.
+struct CausalRow { int r, first, n, ctx; };
+__device__ __forceinline__ int causal_cu(const CausalParams& p, int r) {
+  const int x = p.cu[r];
+  return x < 0 ? 0 : x > p.n_tokens ? p.n_tokens : x;
+}
+__device__ __forceinline__ int causal_ctx(const CausalParams& p, int r, int n) {
+  if (!p.ctx) return n;
+  const int x = p.ctx[r];
+  const long long most = static_cast<long long>(p.width) * p.page;
+  return x < 0 ? 0 : x > most ? static_cast<int>(most) : x;
+}
+
+// One warp per row and head: a lane per key for the scores, then lanes over the head for the weighted sum.  Scores, maximum, sum
+// and output in 32 bits.  Every key is read by every row that sees it: simple, not fast.
+template <class T>
+__global__ void __launch_bounds__(128) causal_attention_rows(const __grid_constant__ CausalParams p) {
+  __shared__ float qs[4][256];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long item = static_cast<long long>(blockIdx.x) * 4 + warp;
+  const int row = static_cast<int>(item / p.H), h = static_cast<int>(item % p.H);
+  if (row >= p.n_tokens || row < causal_cu(p, 0) || row >= causal_cu(p, p.n_req)) return;
+  int a = 0, b = p.n_req;           // last request whose first row is not behind `row`
+  while (b - a > 1) { const int m = (a + b) >> 1; if (causal_cu(p, m) <= row) a = m; else b = m; }
+  const int first = causal_cu(p, a), n = causal_cu(p, a + 1) - first, ctx = causal_ctx(p, a, n);
+  const int seen = ctx - n + (row - first) + 1 < ctx ? ctx - n + (row - first) + 1 : ctx, hk = h / (p.H / p.HK);
+  const T* q = static_cast<const T*>(p.q) + row * p.q_ts + h * p.q_hs;
+  for (int d = lane; d < p.D; d += 32) qs[warp][d] = rope_load(q[d]) * p.scale;
+  __syncwarp();
+  const T* k = static_cast<const T*>(p.k) + hk * p.k_hs;
+  const T* v = static_cast<const T*>(p.v) + hk * p.v_hs;
+  float m = -INFINITY, l = 0.f, acc[8] = {};
+  for (int j0 = 0; j0 < seen; j0 += 32) {
+    const int j = j0 + lane, cnt = seen - j0 < 32 ? seen - j0 : 32;
+    long long ko = -1, vo = -1;     // -1: an id outside the pool, whose keys and values count as zeros
+    float s = -INFINITY;
+    if (j < seen) {
+      if (p.ctx) {
+        const int id = p.table[a * p.table_stride + j / p.page];
+        if (id >= 0 && id < p.n_pages) { ko = id * p.k_ps + (j % p.page) * p.k_ts; vo = id * p.v_ps + (j % p.page) * p.v_ts; }
+        else if (p.status) atomicOr(p.status, SERVE_BAD_PAGE);
+      } else { ko = (first + j) * p.k_ts; vo = (first + j) * p.v_ts; }
+      s = 0.f;
+      if (ko >= 0) for (int d = 0; d < p.D; ++d) s = fmaf(qs[warp][d], rope_load(k[ko + d]), s);
+    }
+    float mx = s;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    const float mn = fmaxf(m, mx), corr = m == mn ? 1.f : expf(m - mn);
+    const float w = j < seen ? expf(s - mn) : 0.f;
+    m = mn;
+    float ws = w;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, d);
+    l = l * corr + ws;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= corr;
+    for (int jj = 0; jj < cnt; ++jj) {
+      const float x = __shfl_sync(0xffffffffu, w, jj);
+      const long long off = __shfl_sync(0xffffffffu, vo, jj);
+      if (off < 0) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (e * 32 + lane < p.D) acc[e] = fmaf(x, rope_load(v[off + e * 32 + lane]), acc[e]);
+    }
+  }
+  T* o = static_cast<T*>(p.o) + row * p.o_ts + h * p.o_hs;
+  const float inv = seen > 0 ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) if (e * 32 + lane < p.D) o[e * 32 + lane] = rope_store<T>(acc[e] * inv);
+}
+
+}  // namespace k
+}  // namespace sod2

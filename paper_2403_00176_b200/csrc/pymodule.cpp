@@ -5,7 +5,9 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <climits>
 #include <cstdint>
+#include <cstring>
 #include <new>
 
 #include "../../include/sod2.h"
@@ -184,12 +186,113 @@ PyObject* py_plan_destroy(PyObject*, PyObject* h) {
   Py_RETURN_NONE;
 }
 
+// Arguments of the serving calls by a pattern: i an integer or an address (None: 0), d a number, 3 / 4 a tuple of an address and its
+// strides (None: absent).  Strides of absent tensors are zero.
+struct Arg { int64_t v[4] = {}; double d = 0; bool there = false; };
+bool parse(PyObject* const* a, Py_ssize_t n, const char* pattern, Arg* out) {
+  if (!want(n, static_cast<Py_ssize_t>(std::strlen(pattern)))) return false;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const char kind = pattern[i];
+    if (kind == 'd') {
+      out[i].d = PyFloat_AsDouble(a[i]);
+      if (out[i].d == -1.0 && PyErr_Occurred()) return false;
+    } else if (a[i] == Py_None) {
+    } else if (kind == 'i') {
+      if (!as_i64(a[i], &out[i].v[0])) return false;
+    } else {
+      const Py_ssize_t m = kind - '0';
+      if (!PyTuple_Check(a[i]) || PyTuple_GET_SIZE(a[i]) != m) {
+        PyErr_Format(PyExc_TypeError, "argument %zd: a tuple of an address and %zd strides is wanted", i, m - 1);
+        return false;
+      }
+      for (Py_ssize_t j = 0; j < m; ++j) if (!as_i64(PyTuple_GET_ITEM(a[i], j), &out[i].v[j])) return false;
+      out[i].there = true;
+    }
+  }
+  return true;
+}
+template <class T> T* addr(const Arg& a) { return reinterpret_cast<T*>(static_cast<intptr_t>(a.v[0])); }
+// An int of the C interface: what does not fit becomes a value that every call refuses.
+int narrow(const Arg& a) { return a.v[0] < INT_MIN || a.v[0] > INT_MAX ? INT_MIN : static_cast<int>(a.v[0]); }
+struct RowsArg {
+  sod2_rows r;
+  bool there;
+  explicit RowsArg(const Arg& a) : r{addr<void>(a), a.v[1], a.v[2]}, there(a.there) {}
+  const sod2_rows* get() const { return there ? &r : nullptr; }
+};
+struct PagesArg {
+  sod2_pages r;
+  bool there;
+  explicit PagesArg(const Arg& a) : r{addr<void>(a), a.v[1], a.v[2], a.v[3]}, there(a.there) {}
+  const sod2_pages* get() const { return there ? &r : nullptr; }
+};
+
+// page_tables(sod2_page_tables' arguments) -> status
+PyObject* py_page_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Arg x[18];
+  if (!parse(a, n, "iiiiiiiiiiiiiiiiii", x)) return nullptr;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sod2_page_tables(narrow(x[0]), x[1].v[0], narrow(x[2]), addr<int32_t>(x[3]), addr<int32_t>(x[4]), addr<int32_t>(x[5]), x[6].v[0], addr<int32_t>(x[7]),
+                        addr<int32_t>(x[8]), x[9].v[0], x[10].v[0], addr<int32_t>(x[11]), addr<int32_t>(x[12]), addr<int64_t>(x[13]), addr<int32_t>(x[14]),
+                        addr<int32_t>(x[15]), addr<int32_t>(x[16]), addr<void>(x[17]));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+// rope_store(dtype, tokens, heads, kv heads, dim, pairs, freq, axis, adjacent, positions, axis stride, q, q_out, k, k_out, v, k cache, v cache,
+// pages, page size, slots, status, stream) -> status
+PyObject* py_rope_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Arg x[23];
+  if (!parse(a, n, "iiiiiiiiiii3333344iiiii", x)) return nullptr;
+  const RowsArg q(x[11]), qo(x[12]), k(x[13]), ko(x[14]), v(x[15]);
+  const PagesArg kc(x[16]), vc(x[17]);
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sod2_rope_store(narrow(x[0]), x[1].v[0], narrow(x[2]), narrow(x[3]), narrow(x[4]), narrow(x[5]), addr<double>(x[6]), addr<uint8_t>(x[7]),
+                       narrow(x[8]), addr<int32_t>(x[9]), x[10].v[0], q.get(), qo.get(), k.get(), ko.get(), v.get(), kc.get(), vc.get(), x[18].v[0],
+                       narrow(x[19]), addr<int64_t>(x[20]), addr<int32_t>(x[21]), addr<void>(x[22]));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+// attention_prompt(sod2_attention_prompt's arguments) -> status
+PyObject* py_attention_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Arg x[16];
+  if (!parse(a, n, "iiiiii3333idiiii", x)) return nullptr;
+  const RowsArg q(x[6]), k(x[7]), v(x[8]), o(x[9]);
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sod2_attention_prompt(narrow(x[0]), narrow(x[1]), x[2].v[0], narrow(x[3]), narrow(x[4]), narrow(x[5]), q.get(), k.get(), v.get(), o.get(),
+                             addr<int32_t>(x[10]), static_cast<float>(x[11].d), addr<void>(x[12]), x[13].v[0] < 0 ? 0 : static_cast<size_t>(x[13].v[0]),
+                             addr<int32_t>(x[14]), addr<void>(x[15]));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+// attention_paged(sod2_attention_paged's arguments) -> status
+PyObject* py_attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Arg x[23];
+  if (!parse(a, n, "iiiiiii33ii44iiiiidiiii", x)) return nullptr;
+  const RowsArg q(x[7]), o(x[8]);
+  const PagesArg kc(x[11]), vc(x[12]);
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sod2_attention_paged(narrow(x[0]), narrow(x[1]), x[2].v[0], x[3].v[0], narrow(x[4]), narrow(x[5]), narrow(x[6]), q.get(), o.get(),
+                            addr<int32_t>(x[9]), addr<int32_t>(x[10]), kc.get(), vc.get(), x[13].v[0], narrow(x[14]), addr<int32_t>(x[15]), x[16].v[0],
+                            x[17].v[0], static_cast<float>(x[18].d), addr<void>(x[19]), x[20].v[0] < 0 ? 0 : static_cast<size_t>(x[20].v[0]),
+                            addr<int32_t>(x[21]), addr<void>(x[22]));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f))
 PyMethodDef methods[] = {
     {"bind", FAST(py_bind), METH_FASTCALL, "sod2_bind_dims"},
     {"plan", FAST(py_plan), METH_FASTCALL, "sod2_plan"},
     {"run", FAST(py_run), METH_FASTCALL, "sod2_run (0), sod2_run_graph (1), sod2_run_exact (2)"},
     {"output_shape", FAST(py_output_shape), METH_FASTCALL, "sod2_run_output_shape"},
+    {"page_tables", FAST(py_page_tables), METH_FASTCALL, "sod2_page_tables"},
+    {"rope_store", FAST(py_rope_store), METH_FASTCALL, "sod2_rope_store"},
+    {"attention_prompt", FAST(py_attention_prompt), METH_FASTCALL, "sod2_attention_prompt"},
+    {"attention_paged", FAST(py_attention_paged), METH_FASTCALL, "sod2_attention_paged"},
     {"binding_destroy", py_binding_destroy, METH_O, "sod2_binding_destroy"},
     {"plan_destroy", py_plan_destroy, METH_O, "sod2_plan_destroy"},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,295 @@
+// Operators of a serving loop as direct calls (include/sod2.h): page tables, rotary positions with the store into a paged cache,
+// causal attention over packed prompts and over the cache.  Checks of arguments, choice of kernel, launches.
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <string>
+
+#include "../../include/sod2.h"
+#include "attention_causal.cuh"
+#include "engine.h"
+#include "kernels_paging.cuh"
+
+using namespace sod2;
+
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffffff - 4096;      // rows are counted in 32 bits, tiles of rows included
+
+// The first thing wrong with a call's arguments.
+struct Check {
+  const char* call;
+  sod2_status status = SOD2_OK;
+  std::string msg;
+  explicit Check(const char* c) : call(c) {}
+  bool need(bool ok, sod2_status s, const char* what) {
+    if (!ok && status == SOD2_OK) { status = s; msg = std::string(call) + ": " + what; }
+    return status == SOD2_OK;
+  }
+  sod2_status fail() { set_thread_error(msg); return status; }
+  sod2_status launched() {
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return SOD2_OK;
+    status = SOD2_E_CUDA;
+    msg = std::string(call) + ": launch failed: " + cudaGetErrorString(e);
+    return fail();
+  }
+};
+
+// The device that holds `p` has to be the current one: the stream belongs to it.
+void on_current_device(Check& c, const void* p) {
+  if (c.status != SOD2_OK) return;
+  cudaPointerAttributes at{};
+  int cur = 0;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess || cudaGetDevice(&cur) != cudaSuccess) {
+    cudaGetLastError();
+    c.need(false, SOD2_E_CUDA, "no CUDA device");
+    return;
+  }
+  c.need(at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged, SOD2_E_INVALID_ARG, "an address is not in device memory");
+  c.need(at.type != cudaMemoryTypeDevice || at.device == cur, SOD2_E_INVALID_ARG, "the device that holds the tensors must be the current device");
+}
+
+int elem_size(int dtype) { return dtype == SOD2_DTYPE_F32 ? 4 : dtype == SOD2_DTYPE_BF16 || dtype == SOD2_DTYPE_F16 ? 2 : 0; }
+bool on(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+void check_rows(Check& c, const sod2_rows* r, int esz, const char* what) {
+  c.need(r && r->data, SOD2_E_INVALID_ARG, what);
+  if (c.status != SOD2_OK) return;
+  c.need(r->token_stride >= 0 && r->head_stride >= 0, SOD2_E_BAD_DIM, "negative stride");
+  c.need(on(r->data, esz), SOD2_E_MISALIGNED, "a tensor is not aligned to its elements");
+}
+void check_pages(Check& c, const sod2_pages* r, int esz, const char* what) {
+  c.need(r && r->data, SOD2_E_INVALID_ARG, what);
+  if (c.status != SOD2_OK) return;
+  c.need(r->page_stride >= 0 && r->token_stride >= 0 && r->head_stride >= 0, SOD2_E_BAD_DIM, "negative stride");
+  c.need(on(r->data, esz), SOD2_E_MISALIGNED, "a cache is not aligned to its elements");
+}
+// 16-byte accesses: address and strides
+bool vec16(const sod2_rows* r, int esz) { return !r || (on(r->data, 16) && r->token_stride * esz % 16 == 0 && r->head_stride * esz % 16 == 0); }
+bool vec16(const sod2_pages* r, int esz) {
+  return !r || (on(r->data, 16) && r->page_stride * esz % 16 == 0 && r->token_stride * esz % 16 == 0 && r->head_stride * esz % 16 == 0);
+}
+
+template <class T, int V>
+void launch_rope(const k::RopeParams& p, cudaStream_t st) {
+  const int unit_rows = p.H + p.HK, units = unit_rows * (p.pairs / V + (p.D - 2 * p.pairs) / V);
+  k::RopeParams q = p;
+  // eight units a thread; fewer where that would leave SMs without a CTA, down to a token, whose heads are then shared out
+  const int most = (p.n_tokens + 148 * 4 - 1) / (148 * 4), want = units > 0 ? 2048 / units : 1;
+  q.tile = want < most ? want : most;
+  q.tile = q.tile < 1 ? 1 : q.tile > 32 ? 32 : q.tile;
+  const int gx = (p.n_tokens + q.tile - 1) / q.tile;
+  int gy = gx < 296 ? 296 / gx : 1;
+  const int rounds = (units * q.tile + 255) / 256;
+  gy = gy > rounds ? rounds : gy;
+  k::rope_store_rows<T, V><<<dim3(gx, gy < 1 ? 1 : gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st>>>(q);
+}
+
+struct AttnCall {
+  int dtype, n_heads, n_kv, dim, n_req;
+  int64_t n_tokens;
+  const sod2_rows *q, *out;
+  const int32_t* cu;
+  float scale;
+};
+
+void check_attention(Check& c, const AttnCall& a) {
+  const int esz = elem_size(a.dtype);
+  c.need(esz != 0, SOD2_E_INVALID_ARG, "dtype must be f32, bf16 or f16");
+  c.need(a.n_heads >= 1 && a.n_kv >= 1 && a.n_heads <= 4096 && a.n_heads % a.n_kv == 0, SOD2_E_BAD_DIM, "the heads must be a multiple of the key heads");
+  c.need(a.dim >= 1 && a.dim <= 256, SOD2_E_BAD_DIM, "head size must be 1..256");
+  c.need(a.n_req >= 0 && a.n_tokens >= 0 && a.n_tokens <= kMaxRows && a.n_req <= kMaxRows, SOD2_E_BAD_DIM, "number of requests or tokens");
+  c.need(std::isfinite(a.scale) && a.scale > 0, SOD2_E_INVALID_ARG, "scale must be positive and finite");
+  if (c.status != SOD2_OK || a.n_req == 0 || a.n_tokens == 0) return;
+  check_rows(c, a.q, esz, "null queries");
+  check_rows(c, a.out, esz, "null output");
+  c.need(a.cu != nullptr, SOD2_E_INVALID_ARG, "null cumulative lengths");
+}
+
+void set_common(k::CausalParams& p, const AttnCall& a) {
+  p.q = a.q->data; p.q_ts = a.q->token_stride; p.q_hs = a.q->head_stride;
+  p.o = a.out->data; p.o_ts = a.out->token_stride; p.o_hs = a.out->head_stride;
+  p.cu = a.cu;
+  p.n_req = a.n_req; p.n_tokens = static_cast<int>(a.n_tokens); p.H = a.n_heads; p.HK = a.n_kv; p.D = a.dim;
+  p.scale = a.scale;
+}
+
+void launch_attention(const k::CausalParams& p, int dtype, cudaStream_t st) {
+  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) * p.H + 3) / 4);
+  if (dtype == SOD2_DTYPE_F32) k::causal_attention_rows<float><<<grid, 128, 0, st>>>(p);
+  else if (dtype == SOD2_DTYPE_F16) k::causal_attention_rows<__half><<<grid, 128, 0, st>>>(p);
+  else k::causal_attention_rows<__nv_bfloat16><<<grid, 128, 0, st>>>(p);
+}
+
+// No exception leaves a C entry: messages are strings, which may fail to allocate.
+template <class F>
+sod2_status guarded(F&& f) {
+  try { return f(); } catch (...) { return SOD2_E_INTERNAL; }
+}
+
+}  // namespace
+
+extern "C" sod2_status sod2_page_tables(int n_requests, int64_t max_tokens, int page_size, const int32_t* dev_past, const int32_t* dev_new,
+                                        const int32_t* dev_free_pages, int64_t n_free, const int32_t* dev_free_head, int32_t* dev_table,
+                                        int64_t table_stride, int64_t table_width, int32_t* dev_cu_tokens, int32_t* dev_ctx, int64_t* dev_slots,
+                                        int32_t* dev_positions, int32_t* dev_free_head_out, int32_t* dev_status, void* cuda_stream) {
+  return guarded([&]() -> sod2_status {
+    Check c("sod2_page_tables");
+    c.need(n_requests >= 0 && n_requests <= kMaxRows && max_tokens >= 0 && max_tokens <= kMaxRows, SOD2_E_BAD_DIM, "number of requests or tokens");
+    c.need(page_size >= 1, SOD2_E_BAD_DIM, "page size must be positive");
+    c.need(n_free >= 0 && n_free <= 0x7fffffff, SOD2_E_BAD_DIM, "number of free pages");
+    c.need(table_width >= 0 && table_width <= 0x7fffffff && table_stride >= table_width, SOD2_E_BAD_DIM, "table width or stride");
+    c.need(dev_cu_tokens && dev_free_head_out, SOD2_E_INVALID_ARG, "null output");
+    c.need(max_tokens == 0 || dev_slots, SOD2_E_INVALID_ARG, "null slot map");
+    c.need(n_free == 0 || dev_free_pages, SOD2_E_INVALID_ARG, "null free list");
+    c.need(n_requests == 0 || (dev_past && dev_new && dev_ctx), SOD2_E_INVALID_ARG, "null lengths");
+    c.need(n_requests == 0 || table_width == 0 || dev_table, SOD2_E_INVALID_ARG, "null table");
+    // CTAs read the lengths and the head while others write their outputs
+    c.need(dev_free_head_out != dev_free_head && (!dev_ctx || (dev_ctx != dev_past && dev_ctx != dev_new)), SOD2_E_INVALID_ARG, "an output is an input");
+    on_current_device(c, dev_cu_tokens);
+    if (c.status != SOD2_OK) return c.fail();
+    k::PageTableParams p{};
+    p.past = dev_past; p.fresh = dev_new; p.free_pages = dev_free_pages; p.free_head = dev_free_head;
+    p.table = dev_table; p.cu = dev_cu_tokens; p.ctx = dev_ctx; p.slots = reinterpret_cast<long long*>(dev_slots);
+    p.positions = dev_positions; p.head_out = dev_free_head_out; p.status = dev_status;
+    p.table_stride = table_stride; p.n_req = n_requests; p.cap = static_cast<int>(max_tokens); p.page = page_size;
+    p.n_free = static_cast<int>(n_free); p.width = static_cast<int>(table_width);
+    // a CTA per tile of rows; with few rows still one per eight requests, up to one per SM, for the tables
+    int grid = static_cast<int>((max_tokens + k::PT_TILE - 1) / k::PT_TILE);
+    const int by_req = (n_requests + 7) / 8 < 148 ? (n_requests + 7) / 8 : 148;
+    grid = grid < by_req ? by_req : grid;
+    k::page_tables<<<grid < 1 ? 1 : grid, k::PT_THREADS, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+    return c.launched();
+  });
+}
+
+extern "C" sod2_status sod2_rope_store(int dtype, int64_t n_tokens, int n_heads, int n_kv_heads, int head_dim, int n_pairs, const double* freq,
+                                       const uint8_t* axis, int adjacent, const int32_t* dev_positions, int64_t axis_stride, const sod2_rows* q,
+                                       const sod2_rows* q_out, const sod2_rows* k, const sod2_rows* k_out, const sod2_rows* v,
+                                       const sod2_pages* k_cache, const sod2_pages* v_cache, int64_t n_pages, int page_size,
+                                       const int64_t* dev_slots, int32_t* dev_status, void* cuda_stream) {
+  return guarded([&]() -> sod2_status {
+    Check c("sod2_rope_store");
+    const int esz = elem_size(dtype);
+    c.need(esz != 0, SOD2_E_INVALID_ARG, "dtype must be f32, bf16 or f16");
+    c.need(n_tokens >= 0 && n_tokens <= kMaxRows, SOD2_E_BAD_DIM, "number of tokens");
+    c.need(n_heads >= 0 && n_heads <= 4096 && n_kv_heads >= 0 && n_kv_heads <= 4096, SOD2_E_BAD_DIM, "number of heads");
+    c.need(head_dim >= 2 && head_dim <= 256, SOD2_E_BAD_DIM, "head size must be 2..256");
+    c.need(n_pairs >= 1 && 2 * n_pairs <= head_dim, SOD2_E_BAD_DIM, "rotated pairs must fit the head");
+    c.need(freq && axis, SOD2_E_INVALID_ARG, "null frequencies");
+    c.need(adjacent == 0 || adjacent == 1, SOD2_E_INVALID_ARG, "adjacent must be 0 or 1");
+    c.need(axis_stride >= 0, SOD2_E_BAD_DIM, "negative stride");
+    c.need((n_heads > 0) == (q != nullptr) && (q != nullptr) == (q_out != nullptr), SOD2_E_INVALID_ARG, "queries come with their heads and their output");
+    c.need((n_kv_heads > 0) == (k != nullptr), SOD2_E_INVALID_ARG, "keys come with their heads");
+    c.need((k != nullptr) == (k_out || k_cache), SOD2_E_INVALID_ARG, "keys come with an output or a cache");
+    c.need((v != nullptr) == (v_cache != nullptr) && (!v || k), SOD2_E_INVALID_ARG, "values come with keys and a cache");
+    c.need(q || k, SOD2_E_INVALID_ARG, "neither queries nor keys");
+    if (q) { check_rows(c, q, esz, "null queries"); check_rows(c, q_out, esz, "null query output"); }
+    if (k) check_rows(c, k, esz, "null keys");
+    if (k_out) check_rows(c, k_out, esz, "null key output");
+    if (v) check_rows(c, v, esz, "null values");
+    if (k_cache) check_pages(c, k_cache, esz, "null key cache");
+    if (v_cache) check_pages(c, v_cache, esz, "null value cache");
+    if (k_cache || v_cache) {
+      c.need(dev_slots != nullptr, SOD2_E_INVALID_ARG, "a cache comes with slots");
+      c.need(page_size >= 1 && n_pages >= 0 && n_pages <= INT64_MAX / page_size, SOD2_E_BAD_DIM, "pages of the cache");
+    }
+    c.need(dev_positions != nullptr, SOD2_E_INVALID_ARG, "null positions");
+    if (c.status == SOD2_OK) for (int j = 0; j < n_pairs; ++j) c.need(std::isfinite(freq[j]), SOD2_E_INVALID_ARG, "a frequency is not finite");
+    if (c.status == SOD2_OK && n_tokens == 0) return SOD2_OK;
+    if (c.status == SOD2_OK) on_current_device(c, q ? q_out->data : k->data);
+    if (c.status != SOD2_OK) return c.fail();
+    k::RopeParams p{};
+    if (q) {
+      p.q = q->data; p.q_ts = q->token_stride; p.q_hs = q->head_stride;
+      p.q_out = q_out->data; p.qo_ts = q_out->token_stride; p.qo_hs = q_out->head_stride;
+    }
+    if (k) { p.k = k->data; p.k_ts = k->token_stride; p.k_hs = k->head_stride; }
+    if (k_out) { p.k_out = k_out->data; p.ko_ts = k_out->token_stride; p.ko_hs = k_out->head_stride; }
+    if (v) { p.v = v->data; p.v_ts = v->token_stride; p.v_hs = v->head_stride; }
+    if (k_cache) { p.kc = k_cache->data; p.kc_ps = k_cache->page_stride; p.kc_ts = k_cache->token_stride; p.kc_hs = k_cache->head_stride; }
+    if (v_cache) { p.vc = v_cache->data; p.vc_ps = v_cache->page_stride; p.vc_ts = v_cache->token_stride; p.vc_hs = v_cache->head_stride; }
+    p.slots = reinterpret_cast<const long long*>(dev_slots); p.positions = dev_positions; p.pos_stride = axis_stride; p.status = dev_status;
+    p.n_slots = k_cache || v_cache ? n_pages * page_size : 0;
+    p.n_tokens = static_cast<int>(n_tokens); p.H = n_heads; p.HK = n_kv_heads; p.D = head_dim; p.pairs = n_pairs; p.adjacent = adjacent;
+    p.page = page_size;
+    for (int j = 0; j < n_pairs; ++j) { p.turns[j] = freq[j] / 6.283185307179586476925; p.axis[j] = axis[j]; }
+    const int V = 16 / esz;
+    const bool vec = head_dim % V == 0 && n_pairs % V == 0 && vec16(q, esz) && vec16(q_out, esz) && vec16(k, esz) && vec16(k_out, esz) &&
+                     vec16(v, esz) && vec16(k_cache, esz) && vec16(v_cache, esz);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == SOD2_DTYPE_F32) { if (vec) launch_rope<float, 4>(p, st); else launch_rope<float, 1>(p, st); }
+    else if (dtype == SOD2_DTYPE_F16) { if (vec) launch_rope<__half, 8>(p, st); else launch_rope<__half, 1>(p, st); }
+    else { if (vec) launch_rope<__nv_bfloat16, 8>(p, st); else launch_rope<__nv_bfloat16, 1>(p, st); }
+    return c.launched();
+  });
+}
+
+extern "C" sod2_status sod2_attention_workspace_bytes(int n_heads, int n_kv_heads, int head_dim, size_t* bytes) {
+  return guarded([&]() -> sod2_status {
+    Check c("sod2_attention_workspace_bytes");
+    c.need(bytes != nullptr, SOD2_E_INVALID_ARG, "null result");
+    c.need(n_heads >= 1 && n_kv_heads >= 1 && n_heads <= 4096 && n_heads % n_kv_heads == 0, SOD2_E_BAD_DIM, "the heads must be a multiple of the key heads");
+    c.need(head_dim >= 1 && head_dim <= 256, SOD2_E_BAD_DIM, "head size must be 1..256");
+    if (c.status != SOD2_OK) return c.fail();
+    *bytes = 256;
+    return SOD2_OK;
+  });
+}
+
+extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t n_tokens, int n_heads, int n_kv_heads, int head_dim,
+                                             const sod2_rows* q, const sod2_rows* k, const sod2_rows* v, const sod2_rows* out,
+                                             const int32_t* dev_cu_tokens, float scale, void* dev_workspace, size_t workspace_bytes,
+                                             int32_t* dev_status, void* cuda_stream) {
+  return guarded([&]() -> sod2_status {
+    Check c("sod2_attention_prompt");
+    const AttnCall a{dtype, n_heads, n_kv_heads, head_dim, n_requests, n_tokens, q, out, dev_cu_tokens, scale};
+    check_attention(c, a);
+    if (c.status == SOD2_OK && (n_requests == 0 || n_tokens == 0)) return SOD2_OK;
+    check_rows(c, k, elem_size(dtype), "null keys");
+    check_rows(c, v, elem_size(dtype), "null values");
+    c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k->data && out->data != v->data), SOD2_E_INVALID_ARG, "the output is an input");
+    if (c.status == SOD2_OK) on_current_device(c, out->data);
+    if (c.status != SOD2_OK) return c.fail();
+    k::CausalParams p{};
+    set_common(p, a);
+    p.k = k->data; p.k_ts = k->token_stride; p.k_hs = k->head_stride;
+    p.v = v->data; p.v_ts = v->token_stride; p.v_hs = v->head_stride;
+    p.status = dev_status;
+    launch_attention(p, dtype, static_cast<cudaStream_t>(cuda_stream));
+    return c.launched();
+  });
+}
+
+extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n_tokens, int64_t max_new, int n_heads, int n_kv_heads,
+                                            int head_dim, const sod2_rows* q, const sod2_rows* out, const int32_t* dev_cu_tokens,
+                                            const int32_t* dev_ctx, const sod2_pages* k_cache, const sod2_pages* v_cache, int64_t n_pages,
+                                            int page_size, const int32_t* dev_table, int64_t table_stride, int64_t table_width, float scale,
+                                            void* dev_workspace, size_t workspace_bytes, int32_t* dev_status, void* cuda_stream) {
+  return guarded([&]() -> sod2_status {
+    Check c("sod2_attention_paged");
+    const AttnCall a{dtype, n_heads, n_kv_heads, head_dim, n_requests, n_tokens, q, out, dev_cu_tokens, scale};
+    check_attention(c, a);
+    c.need(max_new >= 0, SOD2_E_BAD_DIM, "negative bound on the new tokens");
+    c.need(page_size >= 1 && n_pages >= 0 && n_pages <= 0x7fffffff, SOD2_E_BAD_DIM, "pages of the cache");
+    c.need(table_width >= 0 && table_width <= 0x7fffffff && table_stride >= table_width, SOD2_E_BAD_DIM, "table width or stride");
+    if (c.status == SOD2_OK && (n_requests == 0 || n_tokens == 0)) return SOD2_OK;
+    check_pages(c, k_cache, elem_size(dtype), "null key cache");
+    check_pages(c, v_cache, elem_size(dtype), "null value cache");
+    c.need(dev_ctx != nullptr, SOD2_E_INVALID_ARG, "null contexts");
+    c.need(table_width == 0 || dev_table, SOD2_E_INVALID_ARG, "null table");
+    c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k_cache->data && out->data != v_cache->data), SOD2_E_INVALID_ARG, "the output is an input");
+    if (c.status == SOD2_OK) on_current_device(c, out->data);
+    if (c.status != SOD2_OK) return c.fail();
+    k::CausalParams p{};
+    set_common(p, a);
+    p.k = k_cache->data; p.k_ps = k_cache->page_stride; p.k_ts = k_cache->token_stride; p.k_hs = k_cache->head_stride;
+    p.v = v_cache->data; p.v_ps = v_cache->page_stride; p.v_ts = v_cache->token_stride; p.v_hs = v_cache->head_stride;
+    p.ctx = dev_ctx; p.table = dev_table; p.table_stride = table_stride; p.width = static_cast<int>(table_width);
+    p.page = page_size; p.n_pages = static_cast<int>(n_pages); p.status = dev_status;
+    launch_attention(p, dtype, static_cast<cudaStream_t>(cuda_stream));
+    return c.launched();
+  });
+}
