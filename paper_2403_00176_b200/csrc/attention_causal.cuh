@@ -40,22 +40,12 @@ __device__ __forceinline__ int causal_ctx(const CausalParams& p, int r, int n) {
   return x < 0 ? 0 : x > most ? static_cast<int>(most) : x;
 }
 
-// One warp per row and head: a lane per key for the scores, then lanes over the head for the weighted sum.  Scores, maximum, sum
-// and output in 32 bits.  Every key is read by every row that sees it: simple, not fast.
+// One row of one head by a warp: a lane per key for the scores, then lanes over the head for the weighted sum.  Scores, maximum, sum
+// and output in 32 bits.  `seen`: keys of the request that the row sees; none, and the row is zero.
 template <class T>
-__global__ void __launch_bounds__(128) causal_attention_rows(const __grid_constant__ CausalParams p) {
-  __shared__ float qs[4][256];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long item = static_cast<long long>(blockIdx.x) * 4 + warp;
-  const int row = static_cast<int>(item / p.H), h = static_cast<int>(item % p.H);
-  if (row >= p.n_tokens || row < causal_cu(p, 0) || row >= causal_cu(p, p.n_req)) return;
-  int a = 0, b = p.n_req;           // last request whose first row is not behind `row`
-  while (b - a > 1) { const int m = (a + b) >> 1; if (causal_cu(p, m) <= row) a = m; else b = m; }
-  const int first = causal_cu(p, a), n = causal_cu(p, a + 1) - first, ctx = causal_ctx(p, a, n);
-  const int seen = ctx - n + (row - first) + 1 < ctx ? ctx - n + (row - first) + 1 : ctx, hk = h / (p.H / p.HK);
+__device__ __noinline__ void causal_row(const CausalParams& p, int request, int first, int row, int h, int seen) {
+  const int lane = threadIdx.x & 31, hk = h / (p.H / p.HK);
   const T* q = static_cast<const T*>(p.q) + row * p.q_ts + h * p.q_hs;
-  for (int d = lane; d < p.D; d += 32) qs[warp][d] = rope_load(q[d]) * p.scale;
-  __syncwarp();
   const T* k = static_cast<const T*>(p.k) + hk * p.k_hs;
   const T* v = static_cast<const T*>(p.v) + hk * p.v_hs;
   float m = -INFINITY, l = 0.f, acc[8] = {};
@@ -65,12 +55,13 @@ __global__ void __launch_bounds__(128) causal_attention_rows(const __grid_consta
     float s = -INFINITY;
     if (j < seen) {
       if (p.ctx) {
-        const int id = p.table[a * p.table_stride + j / p.page];
+        const int id = p.table[request * p.table_stride + j / p.page];
         if (id >= 0 && id < p.n_pages) { ko = id * p.k_ps + (j % p.page) * p.k_ts; vo = id * p.v_ps + (j % p.page) * p.v_ts; }
         else if (p.status) atomicOr(p.status, SERVE_BAD_PAGE);
       } else { ko = (first + j) * p.k_ts; vo = (first + j) * p.v_ts; }
       s = 0.f;
-      if (ko >= 0) for (int d = 0; d < p.D; ++d) s = fmaf(qs[warp][d], rope_load(k[ko + d]), s);
+      if (ko >= 0) for (int d = 0; d < p.D; ++d) s = fmaf(rope_load(q[d]), rope_load(k[ko + d]), s);
+      s *= p.scale;
     }
     float mx = s;
 #pragma unroll
@@ -96,6 +87,18 @@ __global__ void __launch_bounds__(128) causal_attention_rows(const __grid_consta
   const float inv = seen > 0 ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) if (e * 32 + lane < p.D) o[e * 32 + lane] = rope_store<T>(acc[e] * inv);
+}
+
+// A warp per row and head.  Every key is read by every row that sees it: simple, not fast.
+template <class T>
+__global__ void __launch_bounds__(128) causal_attention_rows(const __grid_constant__ CausalParams p) {
+  const long long item = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  const int row = static_cast<int>(item / p.H), h = static_cast<int>(item % p.H);
+  if (row >= p.n_tokens || row < causal_cu(p, 0) || row >= causal_cu(p, p.n_req)) return;
+  int a = 0, b = p.n_req;           // last request whose first row is not behind `row`
+  while (b - a > 1) { const int m = (a + b) >> 1; if (causal_cu(p, m) <= row) a = m; else b = m; }
+  const int first = causal_cu(p, a), n = causal_cu(p, a + 1) - first, ctx = causal_ctx(p, a, n), seen = ctx - n + (row - first) + 1;
+  causal_row<T>(p, a, first, row, h, seen < ctx ? seen : ctx);
 }
 
 }  // namespace k

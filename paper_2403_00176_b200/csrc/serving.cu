@@ -8,8 +8,10 @@
 
 #include "../../include/sod2.h"
 #include "attention_causal.cuh"
+#include "attention_causal_tcgen05.cuh"
 #include "engine.h"
 #include "kernels_paging.cuh"
+#include "tmap.h"
 
 using namespace sod2;
 
@@ -116,7 +118,79 @@ void set_common(k::CausalParams& p, const AttnCall& a) {
   p.scale = a.scale;
 }
 
-void launch_attention(const k::CausalParams& p, int dtype, cudaStream_t st) {
+// Workspace of the tcgen05 form: two slots per CTA for the parts of cut items, then their descriptions.
+size_t part_floats(int dp) { return static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * dp; }
+size_t workspace_need(int dim) {
+  if (dim > 128 || dim % 8) return 256;
+  const int dp = dim <= 64 ? 64 : 128;
+  return part_floats(dp) * 4 + static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * sizeof(float2) + 2 * k::CTC_GRID * sizeof(int4) + 256;
+}
+
+template <class T, int DP>
+cudaError_t launch_ctc(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& p, cudaStream_t st) {
+  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
+  if (once != cudaSuccess) return once;
+  k::causal_attention_tcgen05<T, DP><<<k::CTC_GRID, k::CTC_THREADS, k::CtcShape<DP>::SMEM, st>>>(q, kk, v, p);
+  if (!p.cut) return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(k::CTC_GRID, 8);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k::causal_join<T, DP>, p);
+}
+
+// max_keys: the host's bound on the keys of a request.  False where the tensor maps cannot express the operands.
+bool tcgen05_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_keys, void* ws, cudaStream_t st) {
+  const bool f16 = dtype == SOD2_DTYPE_F16;
+  const int G = p.H / p.HK;
+  auto on16 = [](const void* a) { return reinterpret_cast<uintptr_t>(a) % 16 == 0; };
+  if (dtype == SOD2_DTYPE_F32 || p.D > 128 || p.D % 8 || G > 128 || !on16(p.q) || !on16(p.k) || !on16(p.v) || !on16(p.o)) return false;
+  if ((p.o_ts | p.o_hs | p.q_ts | p.q_hs | p.k_ps | p.k_ts | p.k_hs | p.v_ps | p.v_ts | p.v_hs) % 8) return false;
+  if (p.ctx && (p.page % 8 || p.n_pages == 0 || p.width == 0)) return false;
+  k::CtcParams a{};
+  a.c = p;
+  a.scale_log2e = p.scale * 1.4426950408889634f;
+  a.G = G;
+  a.tok = 128 / G;
+  a.ksteps = (p.D + 15) / 16;
+  a.n_pv = a.ksteps * 16;
+  a.box_rows = 128;
+  if (p.ctx) { int r = p.page & -p.page; a.box_rows = r < 128 ? r : 128; }    // the largest power of two that pages and blocks share
+  const int dp = p.D <= 64 ? 64 : 128;
+  a.cut = max_keys > (2 * k::CTC_SNAP - 1) * k::CTC_KB;
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  a.desc = reinterpret_cast<int4*>(w);
+  w += 2 * k::CTC_GRID * sizeof(int4);
+  a.part_ml = reinterpret_cast<float2*>(w);
+  w += static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * sizeof(float2);
+  a.part_o = reinterpret_cast<float*>(w);
+  const uint64_t T = p.n_tokens, D = p.D, HK = p.HK;
+  CUtensorMap mq, mk, mv;
+  const uint64_t qe[4] = {D, static_cast<uint64_t>(G), T, HK}, qs[3] = {uint64_t(p.q_hs) * 2, uint64_t(p.q_ts) * 2, uint64_t(p.q_hs) * 2 * G};
+  const uint32_t qb[4] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(a.tok), 1}, kb[4] = {64, static_cast<uint32_t>(a.box_rows), 1, 1};
+  const uint64_t ke[4] = {D, p.ctx ? uint64_t(p.page) : T, HK, p.ctx ? uint64_t(p.n_pages) : 1};
+  const uint64_t ks[3] = {uint64_t(p.k_ts) * 2, uint64_t(p.k_hs) * 2, uint64_t(p.k_ps) * 2}, vs[3] = {uint64_t(p.v_ts) * 2, uint64_t(p.v_hs) * 2, uint64_t(p.v_ps) * 2};
+  if (!encode_16bit_4d(&mq, f16, p.q, qe, qs, qb) || !encode_16bit_4d(&mk, f16, p.k, ke, ks, kb) || !encode_16bit_4d(&mv, f16, p.v, ke, vs, kb)) return false;
+  cudaError_t e;
+  if (f16) e = dp == 64 ? launch_ctc<__half, 64>(mq, mk, mv, a, st) : launch_ctc<__half, 128>(mq, mk, mv, a, st);
+  else e = dp == 64 ? launch_ctc<__nv_bfloat16, 64>(mq, mk, mv, a, st) : launch_ctc<__nv_bfloat16, 128>(mq, mk, mv, a, st);
+  if (e != cudaSuccess) { cudaGetLastError(); c.need(false, SOD2_E_CUDA, cudaGetErrorString(e)); }
+  return true;
+}
+
+void check_workspace(Check& c, int dim, const void* ws, size_t bytes) {
+  if (c.status != SOD2_OK) return;
+  c.need(ws && bytes >= workspace_need(dim), SOD2_E_ARENA_TOO_SMALL, "workspace smaller than sod2_attention_workspace_bytes");
+  c.need(on(ws, 256), SOD2_E_MISALIGNED, "workspace must be 256-byte aligned");
+}
+
+void launch_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_keys, void* ws, cudaStream_t st) {
+  if (tcgen05_attention(c, p, dtype, max_keys, ws, st)) return;
   const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) * p.H + 3) / 4);
   if (dtype == SOD2_DTYPE_F32) k::causal_attention_rows<float><<<grid, 128, 0, st>>>(p);
   else if (dtype == SOD2_DTYPE_F16) k::causal_attention_rows<__half><<<grid, 128, 0, st>>>(p);
@@ -234,7 +308,7 @@ extern "C" sod2_status sod2_attention_workspace_bytes(int n_heads, int n_kv_head
     c.need(n_heads >= 1 && n_kv_heads >= 1 && n_heads <= 4096 && n_heads % n_kv_heads == 0, SOD2_E_BAD_DIM, "the heads must be a multiple of the key heads");
     c.need(head_dim >= 1 && head_dim <= 256, SOD2_E_BAD_DIM, "head size must be 1..256");
     if (c.status != SOD2_OK) return c.fail();
-    *bytes = 256;
+    *bytes = workspace_need(head_dim);
     return SOD2_OK;
   });
 }
@@ -251,6 +325,7 @@ extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t 
     check_rows(c, k, elem_size(dtype), "null keys");
     check_rows(c, v, elem_size(dtype), "null values");
     c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k->data && out->data != v->data), SOD2_E_INVALID_ARG, "the output is an input");
+    check_workspace(c, head_dim, dev_workspace, workspace_bytes);
     if (c.status == SOD2_OK) on_current_device(c, out->data);
     if (c.status != SOD2_OK) return c.fail();
     k::CausalParams p{};
@@ -258,8 +333,8 @@ extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t 
     p.k = k->data; p.k_ts = k->token_stride; p.k_hs = k->head_stride;
     p.v = v->data; p.v_ts = v->token_stride; p.v_hs = v->head_stride;
     p.status = dev_status;
-    launch_attention(p, dtype, static_cast<cudaStream_t>(cuda_stream));
-    return c.launched();
+    launch_attention(c, p, dtype, n_tokens, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
+    return c.status != SOD2_OK ? c.fail() : c.launched();
   });
 }
 
@@ -281,6 +356,7 @@ extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n
     c.need(dev_ctx != nullptr, SOD2_E_INVALID_ARG, "null contexts");
     c.need(table_width == 0 || dev_table, SOD2_E_INVALID_ARG, "null table");
     c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k_cache->data && out->data != v_cache->data), SOD2_E_INVALID_ARG, "the output is an input");
+    check_workspace(c, head_dim, dev_workspace, workspace_bytes);
     if (c.status == SOD2_OK) on_current_device(c, out->data);
     if (c.status != SOD2_OK) return c.fail();
     k::CausalParams p{};
@@ -289,7 +365,7 @@ extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n
     p.v = v_cache->data; p.v_ps = v_cache->page_stride; p.v_ts = v_cache->token_stride; p.v_hs = v_cache->head_stride;
     p.ctx = dev_ctx; p.table = dev_table; p.table_stride = table_stride; p.width = static_cast<int>(table_width);
     p.page = page_size; p.n_pages = static_cast<int>(n_pages); p.status = dev_status;
-    launch_attention(p, dtype, static_cast<cudaStream_t>(cuda_stream));
-    return c.launched();
+    launch_attention(c, p, dtype, table_width * page_size, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
+    return c.status != SOD2_OK ? c.fail() : c.launched();
   });
 }

@@ -100,4 +100,24 @@ inline bool encode_bf16_planes(CUtensorMap* tm, const void* base, uint64_t plane
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Four extents of 16-bit elements (bf16 or f16), strides of the outer three in bytes; box of up to 64 elements by box[1..3], 128-byte
+// swizzle.  An extent of 1 may have any stride.  Returns false where a map cannot express it.
+inline bool encode_16bit_4d(CUtensorMap* tm, bool f16, const void* base, const uint64_t ext[4], const uint64_t stride_bytes[3], const uint32_t box[4]) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t b[4], estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    if (ext[i] == 0 || ext[i] > (uint64_t(1) << 32) || box[i] == 0 || box[i] > 256) return false;
+    dims[i] = ext[i]; b[i] = box[i];
+  }
+  for (int i = 0; i < 3; ++i) {
+    strides[i] = ext[i + 1] == 1 ? (ext[0] * 2 + 15) / 16 * 16 : stride_bytes[i];
+    if (strides[i] == 0 || strides[i] % 16 || strides[i] >= (uint64_t(1) << 40)) return false;
+  }
+  return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, b, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace sod2
