@@ -9,27 +9,32 @@
 //   O += P V       tcgen05.mma with A in TMEM; V is the natural [key, d] tile, used as an MN-major B operand
 // While one tile is in its exponentials the tensor pipe works for the other.  P lies over S (512 columns hold two of S and
 // two of O), so a tile's next S waits for its last product by commit: the order of two MMAs on different accumulators is not
-// documented.  Each tile has an issuing warp of its own, so that this wait holds up nobody else.
+// documented.  One warp issues for both tiles, a product and the tile's next S at a time (see there).
 //
 // Scores, maximum, sum and O are 32-bit; P is rounded to the type of the values (the product's operand type), once.  The exponent
 // reference m moves only when a row's maximum exceeds it by more than 2^8 after scaling: O is rescaled rarely, and always
 // between two products, since S of a block is issued behind the products of the blocks before.
 //
-// Work is divided evenly over the CTAs (one per SM): items are laid end to end, an item weighing its blocks of keys and one
-// more for its start and end, and cut into equal shares.  A cut inside an item makes two parts; each leaves its O, m and l in
+// Work is divided evenly over the CTAs (one per SM): items are laid end to end, an item weighing its blocks of keys and
+// CTC_START more for its start and end, and cut into equal shares.  A cut inside an item makes two parts; each leaves its O, m and l in
 // the workspace and causal_join puts them together.  Cuts near an item's ends move there.  All lengths are on the device, so every
 // CTA works the division out itself: prefix sums over the requests, then a search.
 //
 // Keys behind a row's last are masked by selection before the maximum.  Values behind the request's last key may be anything: their rows of
 // V in shared memory are zeroed before the product.  A value inside the request but behind a row's last key meets a probability of
 // zero, which leaves it out unless it is not finite; a row whose result is not finite is therefore computed again key by key
-// (causal_row).  Rows of a tile without a token, and tiles without one, are computed on whatever is there and never stored.
+// (causal_row).  Rows of a tile without a token are computed on whatever is there and never stored.
 //
-// Warps: 0..3 softmax of tile A, 4..7 of tile B, 8 loads Q and K, 9 loads V, 10 / 11 issue the MMAs of A / B.  A box of the cache
-// is the part of a page that lies in a block; lanes issue boxes side by side: a lane on its own sustains one per 440 cycles
-// (16 rows: 1.3 TB/s over the GPU), 16 lanes of two warps 6.5 TB/s.  Every wait is bounded (ptx.cuh).
+// Other shapes that were built and measured (8192 tokens, 32 heads of 128 over 8; this one 1034 TFLOP/s): one tile per CTA with two
+// warpgroups taking blocks in turn, S and P double buffered (974), the same with three warpgroups and P over S (908).  They
+// keep the tensor pipe and the exponentials apart better, but take in twice the keys and values per row.
+//
+// Warps: 0..3 softmax of tile A, 4..7 of tile B, 8 loads Q and K, 9 loads V, 10 issues the MMAs.  A box of the cache is the part of a
+// page that lies in a block; lanes issue boxes side by side: a lane on its own sustains one per 440 cycles (16 rows: 1.3 TB/s
+// over the GPU), 16 lanes of two warps 6.5 TB/s.  Every wait is bounded (ptx.cuh).
 #pragma once
 #include <cuda.h>
+#include <type_traits>
 #include "attention_causal.cuh"
 #include "ptx.cuh"
 
@@ -41,6 +46,8 @@ constexpr int CTC_GRID = 148;              // CTAs of the division: one per SM
 constexpr int CTC_KB = 128;                // keys per block
 constexpr int CTC_CHUNK = 128 * 128;       // bytes of 128 rows x 64 elements
 constexpr int CTC_PLAN = CTC_THREADS;      // requests per step of the division
+constexpr int CTC_START = 3;               // weight of an item's start and end, in blocks (1: 908, 2: 1015, 3: 1034 TFLOP/s at 8192 tokens; the first
+                                           // items of a head are the shortest, and their CTAs end last where it is too low)
 constexpr int CTC_SNAP = 2;                // blocks: cuts closer than this to an item's ends move there
 
 struct CtcParams {
@@ -52,14 +59,14 @@ struct CtcParams {
   int cut;                    // 1: items may be cut (the workspace is there)
   float* part_o;              // [2 * CTC_GRID slots][2 tiles][DP][128 rows]
   float2* part_ml;            // [2 * CTC_GRID slots][2 tiles][128 rows]: reference (log2) and sum
-  int4* desc;                 // [2 * CTC_GRID]: state (0 none, 1 part, 2 part that ends the item), request, key head, tile pair
+  int4* desc;                 // [2 * CTC_GRID]: state (0 none, 1 part, 2 part that ends the item), request, key head, item of the head
 };
 
 template <int DP> struct CtcShape {
   static constexpr int NC = DP / 64;                    // 64-element chunks of a row
   static constexpr int TILE = NC * CTC_CHUNK;           // bytes of a Q, K or V tile
-  static constexpr int ST = DP == 128 ? 5 : 8;          // K and V tiles in flight
-  static constexpr int SMEM = (2 + ST) * TILE + 1024 /*align*/ + 1024 /*barriers, plan*/;
+  static constexpr int KS = DP == 128 ? 2 : 4, VS = DP == 128 ? 3 : 4;      // K and V tiles in flight: a V tile stays until its block's product
+  static constexpr int SMEM = (2 + KS + VS) * TILE + 512 /*barriers, division*/;
   static constexpr uint32_t TM_S = 0, TM_O = 256;       // columns: S (and P) at 128 per tile, O at DP per tile
 };
 
@@ -78,13 +85,13 @@ __device__ __forceinline__ int ctc_blocks(const CtcReq& q, int end) {
   const int v = q.past + (end < q.n ? end : q.n);
   return v > 0 ? (v + CTC_KB - 1) / CTC_KB : 0;
 }
-__device__ __forceinline__ int ctc_pairs(const CtcReq& q, int tok) { return (q.n + 2 * tok - 1) / (2 * tok); }
+__device__ __forceinline__ int ctc_items(const CtcReq& q, int tok) { return (q.n + 2 * tok - 1) / (2 * tok); }
 
-struct CtcSpot { long long at, item; int r, head, pair, off; };    // position, its item's first, and where that is
+struct CtcSpot { long long at, item; int r, head, idx, off; };    // position, its item's first, and where that is
 
-// Moves a position inside an item to where it may be cut.  off: 0 the item's start, else blocks ahead of the cut + 1.
+// Moves a position inside an item to where it may be cut.  off: 0 the item's start, else blocks ahead of the cut + CTC_START.
 __device__ __forceinline__ int ctc_snap(int off, int blocks, bool cut) {
-  const int w = blocks + 1, j = off - 1;
+  const int w = blocks + CTC_START, j = off - CTC_START;
   if (off == 0) return 0;
   if (!cut || blocks < 2 * CTC_SNAP) return 2 * off <= w ? 0 : w;
   if (j < CTC_SNAP) return 0;
@@ -92,34 +99,34 @@ __device__ __forceinline__ int ctc_snap(int off, int blocks, bool cut) {
 }
 
 // A role's walk over the CTA's share.
-struct CtcSeg { int r, head, pair, first, n, past, j0, j1; bool starts, ends; };
+struct CtcSeg { int r, head, idx, first, n, past, j0, j1; bool starts, ends; };
 struct CtcWalk {
   long long left;
-  int r, head, pair, off;
+  int r, head, idx, off;
   CtcReq q;
   __device__ __forceinline__ void start(const CtcParams& p, const CtcSpot& a, long long units) {
-    left = units; r = a.r; head = a.head; pair = a.pair; off = a.off;
+    left = units; r = a.r; head = a.head; idx = a.idx; off = a.off;
     q.n = 0;
     if (left > 0) q = ctc_request(p.c, r);
   }
   __device__ __forceinline__ bool next(const CtcParams& p, CtcSeg& s) {
     if (left <= 0) return false;
-    while (pair >= ctc_pairs(q, p.tok)) {
-      pair = 0;
+    while (idx >= ctc_items(q, p.tok)) {
+      idx = 0;
       if (q.n > 0 && ++head < p.c.HK) continue;
       head = 0;
       if (++r >= p.c.n_req) { left = 0; return false; }
       q = ctc_request(p.c, r);
     }
-    const int blocks = ctc_blocks(q, (pair + 1) * 2 * p.tok), w = blocks + 1;
+    const int blocks = ctc_blocks(q, (idx + 1) * 2 * p.tok), w = blocks + CTC_START;
     const int end = left < w - off ? off + static_cast<int>(left) : w;
-    s.r = r; s.head = head; s.pair = pair; s.first = q.first; s.n = q.n; s.past = q.past;
-    s.j0 = off > 0 ? off - 1 : 0;
-    s.j1 = end - 1;                       // end = off + 1 with off = 0: the item's start alone, no block
+    s.r = r; s.head = head; s.idx = idx; s.first = q.first; s.n = q.n; s.past = q.past;
+    s.j0 = off > 0 ? off - CTC_START : 0;
+    s.j1 = end - CTC_START;
     s.starts = off == 0; s.ends = end == w;
     left -= end - off;
     off = 0;
-    ++pair;
+    ++idx;
     return true;
   }
 };
@@ -128,34 +135,36 @@ struct CtcWalk {
 __device__ __forceinline__ CtcSpot ctc_locate(const CtcParams& p, int r, long long start, long long x, bool cut) {
   const int lane = threadIdx.x & 31;
   const CtcReq q = ctc_request(p.c, r);
-  const int np = ctc_pairs(q, p.tok);
+  const int np = ctc_items(q, p.tok);
   long long per = 0;                      // weight of one key head
-  for (int i = lane; i < np; i += 32) per += ctc_blocks(q, (i + 1) * 2 * p.tok) + 1;
+#pragma unroll 1
+  for (int i = lane; i < np; i += 32) per += ctc_blocks(q, (i + 1) * 2 * p.tok) + CTC_START;
 #pragma unroll
   for (int d = 16; d; d >>= 1) per += __shfl_xor_sync(0xffffffffu, per, d);
   CtcSpot s;
   s.r = r; s.at = x;
   s.head = per > 0 ? static_cast<int>((x - start) / per) : 0;
   long long base = start + s.head * per;
+#pragma unroll 1
   for (int i0 = 0; i0 < np; i0 += 32) {
-    const int w = i0 + lane < np ? ctc_blocks(q, (i0 + lane + 1) * 2 * p.tok) + 1 : 0;
+    const int w = i0 + lane < np ? ctc_blocks(q, (i0 + lane + 1) * 2 * p.tok) + CTC_START : 0;
     int inc = w;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(0xffffffffu, inc, d); if (lane >= d) inc += y; }
     const unsigned hit = __ballot_sync(0xffffffffu, x < base + inc);
     if (hit) {
       const int l = __ffs(hit) - 1, wl = __shfl_sync(0xffffffffu, w, l), il = __shfl_sync(0xffffffffu, inc, l);
-      s.pair = i0 + l;
+      s.idx = i0 + l;
       s.item = base + il - wl;
-      const int off = ctc_snap(static_cast<int>(x - s.item), wl - 1, cut);
+      const int off = ctc_snap(static_cast<int>(x - s.item), wl - CTC_START, cut);
       s.at = s.item + off;
       s.off = off;
-      if (off == wl) { s.item = s.at; s.off = 0; ++s.pair; }     // the next item's start; CtcWalk goes on to the next head or request
+      if (off == wl) { s.item = s.at; s.off = 0; ++s.idx; }     // the next item's start; CtcWalk goes on to the next head or request
       return s;
     }
     base += __shfl_sync(0xffffffffu, inc, 31);
   }
-  s.pair = np; s.item = s.at; s.off = 0;
+  s.idx = np; s.item = s.at; s.off = 0;
   return s;
 }
 
@@ -164,26 +173,31 @@ __device__ __forceinline__ void ctc_divide(const CtcParams& p, long long* weight
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   long long total = 0, lo = 0, hi = 0;
   // once for the total, once more for the places of the share's ends (the same chunk, with few requests)
+#pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
     long long base = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < p.c.n_req; r0 += CTC_PLAN) {
       const int nr = p.c.n_req - r0 < CTC_PLAN ? p.c.n_req - r0 : CTC_PLAN;
       if (pass == 0 || p.c.n_req > CTC_PLAN) {
         __syncthreads();
         if (static_cast<int>(threadIdx.x) < nr) {
           const CtcReq q = ctc_request(p.c, r0 + threadIdx.x);
-          const int np = ctc_pairs(q, p.tok);
+          const int np = ctc_items(q, p.tok);
           long long w = 0;
-          if (np <= 64) for (int i = 0; i < np; ++i) w += ctc_blocks(q, (i + 1) * 2 * p.tok) + 1;
+          if (np <= 64)
+#pragma unroll 1
+            for (int i = 0; i < np; ++i) w += ctc_blocks(q, (i + 1) * 2 * p.tok) + CTC_START;
           weight[threadIdx.x] = np <= 64 ? w * p.c.HK : -1;
         }
         __syncthreads();
         for (int i = warp; i < nr; i += CTC_THREADS / 32) {        // long requests: a warp each
           if (weight[i] >= 0) continue;
           const CtcReq q = ctc_request(p.c, r0 + i);
-          const int np = ctc_pairs(q, p.tok);
+          const int np = ctc_items(q, p.tok);
           long long w = 0;
-          for (int t = lane; t < np; t += 32) w += ctc_blocks(q, (t + 1) * 2 * p.tok) + 1;
+#pragma unroll 1
+          for (int t = lane; t < np; t += 32) w += ctc_blocks(q, (t + 1) * 2 * p.tok) + CTC_START;
 #pragma unroll
           for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
           __syncwarp();
@@ -193,6 +207,7 @@ __device__ __forceinline__ void ctc_divide(const CtcParams& p, long long* weight
       }
       // every warp sums the chunk: 12 requests a lane
       long long sum = 0;
+#pragma unroll 1
       for (int e = 0; e < CTC_PLAN / 32; ++e) { const int i = lane * (CTC_PLAN / 32) + e; if (i < nr) sum += weight[i]; }
       long long inc = sum;
 #pragma unroll
@@ -219,7 +234,7 @@ __device__ __forceinline__ void ctc_divide(const CtcParams& p, long long* weight
       hi = total * (blockIdx.x + 1) / gridDim.x;
       if (threadIdx.x == 0) {
         spot[0].at = spot[1].at = total; spot[0].off = spot[1].off = 0; spot[0].item = spot[1].item = total;
-        spot[0].r = spot[1].r = p.c.n_req; spot[0].head = spot[1].head = spot[0].pair = spot[1].pair = 0;
+        spot[0].r = spot[1].r = p.c.n_req; spot[0].head = spot[1].head = spot[0].idx = spot[1].idx = 0;
       }
       __syncthreads();
     }
@@ -231,10 +246,14 @@ __device__ __forceinline__ void ctc_divide(const CtcParams& p, long long* weight
 template <class T> struct CtcType;
 template <> struct CtcType<__nv_bfloat16> {
   static constexpr uint32_t fmt = (1u << 7) | (1u << 10);
+  static constexpr float shift = 0.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
 };
 template <> struct CtcType<__half> {
   static constexpr uint32_t fmt = 0;
+  // P, its sum and O carry a factor 2^7: P stays below 2^15, and is a normal f16 number down to 2^-21 of a row's largest.  (Without it
+  // down to 2^-14; a value that is small for the key that dominates a row then shows the steps of all the others.)
+  static constexpr float shift = 7.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
 };
 // instruction descriptor, kind::f16, 32-bit accumulator, M = 128; mn_b: the B operand is MN-major
@@ -250,15 +269,19 @@ __device__ __forceinline__ float ctc_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float ctc_max32(float mx, const uint32_t* s) {
-  float a = mx, b = -INFINITY;
+// maximum of 128 scores, three operands per instruction, in eight chains
+__device__ __forceinline__ float ctc_max128(const uint32_t* s) {
+  float a[8];
 #pragma unroll
-  for (int e = 0; e < 32; e += 4) {
-    a = fmaxf(fmaxf(a, __uint_as_float(s[e])), __uint_as_float(s[e + 1]));
-    b = fmaxf(fmaxf(b, __uint_as_float(s[e + 2])), __uint_as_float(s[e + 3]));
-  }
-  return fmaxf(a, b);
+  for (int h = 0; h < 8; ++h) a[h] = fmaxf(__uint_as_float(s[h]), __uint_as_float(s[h + 8]));
+#pragma unroll
+  for (int e = 16; e < 128; e += 16)
+#pragma unroll
+    for (int h = 0; h < 8; ++h) a[h] = fmaxf(fmaxf(a[h], __uint_as_float(s[e + h])), __uint_as_float(s[e + h + 8]));
+  return fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7])));
 }
+// 32 probabilities 2^(s c - m c) as 16 packed pairs, their sum added to l.  (One pair in four or eight by a polynomial on the FMA pipe instead:
+// 1047 and 1025 TFLOP/s against 1034 at 8192 tokens, slower on prompts of 1000, where the exponentials are not what is waited for.)
 template <class T>
 __device__ __forceinline__ void ctc_exp32(const uint32_t* s, uint32_t* pk, float2 c2, float2 mc2, float2* l) {
 #pragma unroll
@@ -275,30 +298,37 @@ __global__ void __launch_bounds__(CTC_THREADS, 1)
 causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CtcParams p) {
   using Sh = CtcShape<DP>;
-  constexpr int ST = Sh::ST;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));   // [2 tiles]
-  uint8_t* sKV = sQ + 2 * Sh::TILE;                                                                               // [ST], K and V in turn
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + ST * Sh::TILE);
+  constexpr int KS = Sh::KS, VS = Sh::VS;
+  extern __shared__ __align__(1024) uint8_t ctc_smem[];
+  uint8_t* sQ = ctc_smem;                                               // [2 tiles]
+  uint8_t* sK = sQ + 2 * Sh::TILE;                                      // [KS]
+  uint8_t* sV = sK + KS * Sh::TILE;                                     // [VS]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sV + VS * Sh::TILE);
   uint64_t* q_full = bars;            // [2] per tile: Q landed
   uint64_t* q_free = bars + 2;        // [2] the item's last S is done
   uint64_t* s_full = bars + 4;        // [2] S done
-  uint64_t* p_full = bars + 6;        // [2] P written
-  uint64_t* o_full = bars + 8;        // [2] product done
-  uint64_t* kv_full = bars + 10;      // [ST]
-  uint64_t* kv_free = bars + 10 + ST; // [ST] both tiles are through with it
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 2 * ST);
+  uint64_t* p_half = bars + 6;        // [2] P of the first 64 keys written
+  uint64_t* p_full = bars + 8;        // [2] all of P written
+  uint64_t* o_full = bars + 10;       // [2] product done
+  // K and V have a ring each: one producer's waits then follow its own ring's phases, whatever the other one does
+  uint64_t* k_full = bars + 12;       // [KS]
+  uint64_t* k_free = k_full + KS;     // [KS] both tiles' S are done
+  uint64_t* v_full = k_free + KS;     // [VS]
+  uint64_t* v_free = v_full + VS;     // [VS] both tiles' products are done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_free + VS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  CtcSpot* spot = reinterpret_cast<CtcSpot*>(bars + 12 + 2 * ST);       // [2]
-  long long* weight = reinterpret_cast<long long*>(sKV);                // [CTC_PLAN], ahead of the first load
+  CtcSpot* spot = reinterpret_cast<CtcSpot*>(v_free + VS + 1);          // [2]
+  static_assert((13 + 2 * KS + 2 * VS) * 8 + 2 * sizeof(CtcSpot) <= 512, "");
+  long long* weight = reinterpret_cast<long long*>(sK);                 // [CTC_PLAN], ahead of the first load
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int b = 0; b < 2; ++b) {
-      ptx::mbar_init(&q_full[b], 1); ptx::mbar_init(&q_free[b], 1);
-      ptx::mbar_init(&s_full[b], 1); ptx::mbar_init(&p_full[b], 4); ptx::mbar_init(&o_full[b], 1);
+      ptx::mbar_init(&q_full[b], 1); ptx::mbar_init(&q_free[b], 1); ptx::mbar_init(&s_full[b], 1);
+      ptx::mbar_init(&p_half[b], 4); ptx::mbar_init(&p_full[b], 4); ptx::mbar_init(&o_full[b], 1);
     }
-    for (int b = 0; b < ST; ++b) { ptx::mbar_init(&kv_full[b], 1); ptx::mbar_init(&kv_free[b], 2); }
+    for (int b = 0; b < KS; ++b) { ptx::mbar_init(&k_full[b], 1); ptx::mbar_init(&k_free[b], 1); }
+    for (int b = 0; b < VS; ++b) { ptx::mbar_init(&v_full[b], 1); ptx::mbar_init(&v_free[b], 1); }
     *dead = 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tmap(&tmQ);
@@ -319,9 +349,9 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   if (p.cut && threadIdx.x < 2) {     // what this CTA leaves in its two slots
     int4 d = make_int4(0, 0, 0, 0);
     if (threadIdx.x == 0) {           // the item that an earlier CTA began
-      if (from.off > 0 && units > 0) d = make_int4(to.off > 0 && to.item == from.item ? 1 : 2, from.r, from.head, from.pair);
+      if (from.off > 0 && units > 0) d = make_int4(to.off > 0 && to.item == from.item ? 1 : 2, from.r, from.head, from.idx);
     } else if (to.off > 0 && to.item >= from.at) {                  // the item that this CTA begins and leaves unfinished
-      d = make_int4(1, to.r, to.head, to.pair);
+      d = make_int4(1, to.r, to.head, to.idx);
     }
     p.desc[2 * blockIdx.x + threadIdx.x] = d;
   }
@@ -331,7 +361,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   const int tok = p.tok;
   // blocks of the segment that tile t takes part in
   auto blocks_of = [&](const CtcSeg& g, int t) {
-    const int t0 = (2 * g.pair + t) * tok;
+    const int t0 = (2 * g.idx + t) * tok;
     if (t0 >= g.n) return 0;
     const CtcReq q{g.first, g.n, g.past};
     const int b = ctc_blocks(q, t0 + tok);
@@ -339,139 +369,222 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     return e > g.j0 ? e - g.j0 : 0;
   };
 
-  if (warp == 8 || warp == 9) {
-    // ---- TMA producers: warp 8 Q and the K tiles (even turns of the ring), warp 9 the V tiles (odd ones)
-    const bool is_k = warp == 8;
-    const CUtensorMap* tm = is_k ? &tmK : &tmV;
-    int turn = is_k ? 0 : 1, qn[2] = {0, 0};
-    const int per = CTC_KB / p.box_rows;                  // boxes of 64 columns in a block
-    const int chunk = lane / per, box = lane - chunk * per;
-    const int* table = p.c.table;
-    int bad = 0;
-    while (walk.next(p, s)) {
-      if (is_k) {
-        for (int t = 0; t < 2; ++t) {
-          if (blocks_of(s, t) == 0) continue;
-          if (qn[t] > 0) ptx::mbar_wait_warp(&q_free[t], (qn[t] - 1) & 1, dead);
-          ++qn[t];
-          if (*dead) continue;
-          if (lane == 0) ptx::mbar_expect_tx(&q_full[t], Sh::NC * 128 * tok * p.G);
+  // the 168 registers a thread that the CTA starts with (3 x 168 = 504 for the three warps of a quarter) are shared out: 2 x 208 + 88
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp < 10) {
+      // ---- TMA producers: warp 8 Q and the K tiles, warp 9 the V tiles
+      const bool is_k = warp == 8;
+      const CUtensorMap* tm = is_k ? &tmK : &tmV;
+      uint64_t* full = is_k ? k_full : v_full;
+      uint64_t* free_ = is_k ? k_free : v_free;
+      uint8_t* ring = is_k ? sK : sV;
+      const int stages = is_k ? KS : VS;
+      int stage = 0, use = 0, qn0 = 0, qn1 = 0;
+      const int per = CTC_KB / p.box_rows;                  // boxes of 64 columns in a block
+      const int chunk = lane / per, box = lane - chunk * per;
+      const int* table = p.c.table;
+      int bad = 0;
+#pragma unroll 1
+      while (walk.next(p, s)) {
+        if (is_k) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (blocks_of(s, t) == 0) continue;
+            int& qn = t ? qn1 : qn0;
+            if (qn > 0) ptx::mbar_wait_warp(&q_free[t], (qn - 1) & 1, dead);
+            ++qn;
+            if (!*dead) {
+              if (lane == 0) ptx::mbar_expect_tx(&q_full[t], Sh::NC * 128 * tok * p.G);
+              __syncwarp();
+              if (lane < Sh::NC)
+                ptx::tma_load_4d(sQ + t * Sh::TILE + lane * CTC_CHUNK, &tmQ, lane * 64, 0, s.first + (2 * s.idx + t) * tok, s.head, &q_full[t]);
+            }
+            __syncwarp();
+          }
+        }
+        const int ctx = s.past + s.n;
+        const int* ids = table ? table + s.r * p.c.table_stride : nullptr;
+        // the page of this lane's box, looked up a block ahead
+        auto page_of = [&](int j) {
+          const int row = j * CTC_KB + box * p.box_rows;
+          return chunk < Sh::NC && j < s.j1 && row < ctx ? ids[row / p.c.page] : 0;
+        };
+        int id = table ? page_of(s.j0) : 0;
+#pragma unroll 1
+        for (int j = s.j0; j < s.j1; ++j) {
+          const int row = j * CTC_KB + box * p.box_rows;
+          const bool mine = chunk < Sh::NC && (!table || row < ctx);
+          const int ahead = table ? page_of(j + 1) : 0;
+          if (use > 0) ptx::mbar_wait_warp(&free_[stage], (use - 1) & 1, dead);
+          const int n = __popc(__ballot_sync(0xffffffffu, mine));
+          if (!*dead) {
+            if (lane == 0) ptx::mbar_expect_tx(&full[stage], n * p.box_rows * 128);
+            __syncwarp();
+            if (mine) {
+              uint8_t* dst = ring + stage * Sh::TILE + chunk * CTC_CHUNK + box * p.box_rows * 128;
+              if (table) {
+                int page = id;
+                if (page < 0 || page >= p.c.n_pages) { page = p.c.n_pages; bad = SERVE_BAD_PAGE; }   // outside the map: zeros
+                ptx::tma_load_4d(dst, tm, chunk * 64, row % p.c.page, s.head, page, &full[stage]);
+              } else {
+                ptx::tma_load_4d(dst, tm, chunk * 64, s.first + row, s.head, 0, &full[stage]);
+              }
+            }
+          }
           __syncwarp();
-          if (lane < Sh::NC)
-            ptx::tma_load_4d(sQ + t * Sh::TILE + lane * CTC_CHUNK, &tmQ, lane * 64, 0, s.first + (2 * s.pair + t) * tok, s.head, &q_full[t]);
-          __syncwarp();
+          id = ahead;
+          if (++stage == stages) { stage = 0; ++use; }
         }
       }
-      const int ctx = s.past + s.n;
-      const int* ids = table ? table + s.r * p.c.table_stride : nullptr;
-      // the page of this lane's box, looked up a block ahead
-      auto page_of = [&](int j) {
-        const int row = j * CTC_KB + box * p.box_rows;
-        return chunk < Sh::NC && j < s.j1 && row < ctx ? ids[row / p.c.page] : 0;
-      };
-      int id = table ? page_of(s.j0) : 0;
-      for (int j = s.j0; j < s.j1; ++j, turn += 2) {
-        const int b = turn % ST, use = turn / ST, row = j * CTC_KB + box * p.box_rows;
-        const bool mine = chunk < Sh::NC && (!table || row < ctx);
-        const int ahead = table ? page_of(j + 1) : 0;
-        if (use > 0) ptx::mbar_wait_warp(&kv_free[b], (use - 1) & 1, dead);
-        if (*dead) continue;
-        const int n = __popc(__ballot_sync(0xffffffffu, mine));
-        if (lane == 0) ptx::mbar_expect_tx(&kv_full[b], n * p.box_rows * 128);
-        __syncwarp();
-        if (mine) {
-          uint8_t* dst = sKV + b * Sh::TILE + chunk * CTC_CHUNK + box * p.box_rows * 128;
-          if (table) {
-            int page = id;
-            if (page < 0 || page >= p.c.n_pages) { page = p.c.n_pages; bad = SERVE_BAD_PAGE; }   // outside the map: zeros
-            ptx::tma_load_4d(dst, tm, chunk * 64, row % p.c.page, s.head, page, &kv_full[b]);
-          } else {
-            ptx::tma_load_4d(dst, tm, chunk * 64, s.first + row, s.head, 0, &kv_full[b]);
+      if (bad && p.c.status) atomicOr(p.c.status, bad);
+    } else if (warp == 10) {
+      // ---- MMA issuer: the two tiles in turn, each time the product of a block and behind it S of the tile's next block, if need be of
+      // its next item.  Serving one tile at a time lets one's exponentials run beside the other's MMAs; two issuers of their own,
+      // one a tile, fell into step: both products at once, then both S, then both tiles in their exponentials (8192 tokens,
+      // 32 heads of 128: 4600 cycles per block of both, this way 3640).
+      const ptx::Leader one = ptx::elect_leader();
+      const uint32_t idesc_qk = ctc_idesc<T>(CTC_KB, false), idesc_pv = ctc_idesc<T>(p.n_pv, true);
+      const uint64_t d_q = ptx::smem_desc_sw128(ptx::smem_u32(sQ)), d_k = ptx::smem_desc_sw128(ptx::smem_u32(sK)), d_v = ctc_desc_mn(ptx::smem_u32(sV));
+      int k_stage = 0, k_use = 0, v_stage = 0, v_use = 0;     // of the block whose S / product comes next
+      int items0 = 0, items1 = 0, n0 = 0, n1 = 0;             // items and blocks of each tile so far
+      // S of tile t; free_k: nobody reads the K tile after; last: nor Q
+      auto issue_s = [&](auto tc, bool free_k, bool last) {
+        constexpr int t = decltype(tc)::value;
+        const int n = t ? n1 : n0;
+        const uint64_t dq = d_q + t * (Sh::TILE >> 4), dk = d_k + static_cast<uint64_t>(k_stage * (Sh::TILE >> 4));
+        ptx::mbar_wait_lanes(&k_full[k_stage], k_use & 1, dead);
+        if (n > 0) ptx::mbar_wait_lanes(&o_full[t], (n - 1) & 1, dead);       // P is read: S may be written over it
+        ptx::tc_fence_after();
+        if (p.ksteps == DP / 16) {
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk) {
+            const uint64_t step = (kk >> 2) * (CTC_CHUNK >> 4) + 2 * (kk & 3);
+            ptx::mma_bf16(one, tmem + Sh::TM_S + t * 128, dq + step, dk + step, idesc_qk, kk != 0);
+          }
+        } else {
+#pragma unroll 1
+          for (int kk = 0; kk < p.ksteps; ++kk) {
+            const uint64_t step = (kk >> 2) * (CTC_CHUNK >> 4) + 2 * (kk & 3);
+            ptx::mma_bf16(one, tmem + Sh::TM_S + t * 128, dq + step, dk + step, idesc_qk, kk != 0);
           }
         }
         __syncwarp();
-        id = ahead;
-      }
-    }
-    if (bad && p.c.status) atomicOr(p.c.status, bad);
-  } else if (warp >= 10) {
-    // ---- MMA issuers: S of the next block behind the product of this one
-    const int t = warp - 10;
-    const ptx::Leader one = ptx::elect_leader();
-    const uint32_t idesc_qk = ctc_idesc<T>(CTC_KB, false), idesc_pv = ctc_idesc<T>(p.n_pv, true);
-    const uint32_t tS = tmem + Sh::TM_S + t * 128, tO = tmem + Sh::TM_O + t * DP;
-    const uint64_t dQ = ptx::smem_desc_sw128(ptx::smem_u32(sQ + t * Sh::TILE));
-    int turn = 0, items = 0, n = 0;          // ring turns, items and blocks of this tile so far
-    while (walk.next(p, s)) {
-      const int len = s.j1 - s.j0, mine = blocks_of(s, t);
-      if (mine > 0) { ptx::mbar_wait_warp(&q_full[t], items & 1, dead); ++items; }
-      auto issue_s = [&](int i) {
-        const int b = (turn + 2 * i) % ST, use = (turn + 2 * i) / ST;
-        const uint64_t dK = ptx::smem_desc_sw128(ptx::smem_u32(sKV + b * Sh::TILE));
-        ptx::mbar_wait_lanes(&kv_full[b], use & 1, dead);
-        ptx::tc_fence_after();
-        for (int kk = 0; kk < p.ksteps; ++kk) {
-          const uint64_t step = (kk >> 2) * (CTC_CHUNK >> 4) + 2 * (kk & 3);
-          ptx::mma_bf16(one, tS, dQ + step, dK + step, idesc_qk, kk != 0);
-        }
-        __syncwarp();
         ptx::mma_commit(one, &s_full[t]);
-        ptx::mma_commit(one, &kv_free[b]);
-        if (i + 1 == mine) ptx::mma_commit(one, &q_free[t]);
+        if (free_k) ptx::mma_commit(one, &k_free[k_stage]);
+        if (last) ptx::mma_commit(one, &q_free[t]);
       };
-      auto pass = [&](int i) {                // a tile that this one has no part in
-        const int b = i % ST, use = i / ST;
-        ptx::mbar_wait_warp(&kv_full[b], use & 1, dead);
-        ptx::mbar_arrive_warp(&kv_free[b]);
-      };
-      const int v_end = s.past + ((2 * s.pair + t + 1) * tok < s.n ? (2 * s.pair + t + 1) * tok : s.n);   // keys that the tile sees
-      for (int i = 0; i < len; ++i) {
-        if (i >= mine) { pass(turn + 2 * i); pass(turn + 2 * i + 1); continue; }
-        if (i == 0) issue_s(0);
-        const int b = (turn + 2 * i + 1) % ST, use = (turn + 2 * i + 1) / ST;
-        const uint32_t aV = ptx::smem_u32(sKV + b * Sh::TILE);
-        const int keys = v_end - (s.j0 + i) * CTC_KB, steps = keys < CTC_KB ? (keys + 15) >> 4 : CTC_KB / 16;
-        ptx::mbar_wait_lanes(&kv_full[b], use & 1, dead);
-        ptx::mbar_wait_lanes(&p_full[t], n & 1, dead);
+      // O of tile t from P and the V tile; keys: how many of the block the tile sees
+      auto issue_o = [&](auto tc, int keys, bool first, bool free_v) {
+        constexpr int t = decltype(tc)::value;
+        const int n = t ? n1 : n0;
+        const uint64_t dv = d_v + static_cast<uint64_t>(v_stage * (Sh::TILE >> 4));
+        const uint32_t tS = tmem + Sh::TM_S + t * 128, tO = tmem + Sh::TM_O + t * DP;
+        ptx::mbar_wait_lanes(&v_full[v_stage], v_use & 1, dead);
+        ptx::mbar_wait_lanes(&p_half[t], n & 1, dead);
         ptx::tc_fence_after();
-        for (int kk = 0; kk < steps; ++kk)
-          ptx::mma_bf16_a_tmem(one, tO, tS + kk * 8, ctc_desc_mn(aV + kk * 2048), idesc_pv, (i | kk) != 0);
+        if (keys > CTC_KB - 16) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) ptx::mma_bf16_a_tmem(one, tO, tS + kk * 8, dv + kk * 128, idesc_pv, !first || kk != 0);
+          ptx::mbar_wait_lanes(&p_full[t], n & 1, dead);
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int kk = 4; kk < 8; ++kk) ptx::mma_bf16_a_tmem(one, tO, tS + kk * 8, dv + kk * 128, idesc_pv, 1);
+        } else {
+          ptx::mbar_wait_lanes(&p_full[t], n & 1, dead);
+          ptx::tc_fence_after();
+#pragma unroll 1
+          for (int kk = 0; kk * 16 < keys; ++kk) ptx::mma_bf16_a_tmem(one, tO, tS + kk * 8, dv + kk * 128, idesc_pv, !first || kk != 0);
+        }
         __syncwarp();
         ptx::mma_commit(one, &o_full[t]);
-        ptx::mma_commit(one, &kv_free[b]);
-        if (i + 1 < mine) {
-          ptx::mbar_wait_warp(&o_full[t], n & 1, dead);       // P is read: S may be written over it
-          issue_s(i + 1);
-        }
-        ++n;
+        if (free_v) ptx::mma_commit(one, &v_free[v_stage]);
+        if (t) ++n1; else ++n0;
+      };
+      auto next = [&](CtcSeg& g) {            // the next segment with blocks
+        while (walk.next(p, g)) if (g.j1 > g.j0) return true;
+        return false;
+      };
+      // the first S of a segment of which the tile has `blocks`, tile B `blocks_b`
+      auto first_s = [&](auto tc, int blocks, int blocks_b) {
+        constexpr int t = decltype(tc)::value;
+        if (blocks == 0) return;
+        int& items = t ? items1 : items0;
+        ptx::mbar_wait_warp(&q_full[t], items & 1, dead);
+        ++items;
+        issue_s(tc, t == 1 || blocks_b == 0, blocks == 1);
+      };
+      auto next_k = [&] { if (++k_stage == KS) { k_stage = 0; ++k_use; } };
+      constexpr std::integral_constant<int, 0> A{};
+      constexpr std::integral_constant<int, 1> B{};
+      bool more = next(s);
+      int mine0 = 0, mine1 = 0;
+      if (more) {
+        mine0 = blocks_of(s, 0);
+        mine1 = blocks_of(s, 1);
+        first_s(A, mine0, mine1);
+        first_s(B, mine1, mine1);
+        next_k();
       }
-      turn += 2 * len;
+#pragma unroll 1
+      while (more) {
+        CtcSeg s2;
+        more = next(s2);
+        const int then0 = more ? blocks_of(s2, 0) : 0, then1 = more ? blocks_of(s2, 1) : 0;
+        const int len = s.j1 - s.j0;
+        auto half_turn = [&](auto tc, int i, int mine, int then, int keys) {
+          constexpr int t = decltype(tc)::value;
+          if (i < mine) issue_o(tc, keys, i == 0, t == 1 || i >= mine1);
+          if (i + 1 < mine) issue_s(tc, t == 1 || i + 1 >= mine1, i + 2 == mine);
+          else if (i + 1 == len) first_s(tc, then, then1);
+        };
+        const int t0 = 2 * s.idx * tok;
+        int keys0 = s.past + (t0 + tok < s.n ? t0 + tok : s.n) - s.j0 * CTC_KB, keys1 = s.past + (t0 + 2 * tok < s.n ? t0 + 2 * tok : s.n) - s.j0 * CTC_KB;
+#pragma unroll 1
+        for (int i = 0; i < len; ++i, keys0 -= CTC_KB, keys1 -= CTC_KB) {
+          half_turn(A, i, mine0, then0, keys0);
+          half_turn(B, i, mine1, then1, keys1);
+          next_k();
+          if (++v_stage == VS) { v_stage = 0; ++v_use; }
+        }
+        s = s2;
+        mine0 = then0; mine1 = then1;
+      }
     }
   } else {
     // ---- softmax warps: tile t = warp / 4, a thread per row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int t = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + Sh::TM_S + t * 128, tO = tmem + lane_base + Sh::TM_O + t * DP;
     const float c = p.scale_log2e;
     const int rt = row / p.G, rg = row - rt * p.G;
-    int turn = 0, n = 0;
+    int gb = 0, n = 0;                        // the segment's first block, this tile's blocks so far
+#pragma unroll 1
     while (walk.next(p, s)) {
-      const int len = s.j1 - s.j0, mine = blocks_of(s, t), t0 = (2 * s.pair + t) * tok;
+      const int len = s.j1 - s.j0, mine = blocks_of(s, t), t0 = (2 * s.idx + t) * tok;
       const bool valid = rt < tok && t0 + rt < s.n;
-      const int lim = valid ? s.past + t0 + rt + 1 : 0;       // keys that the row sees
+      // keys that the row sees; rows without a token are computed on whatever is there, unmasked
+      const int lim = valid ? s.past + t0 + rt + 1 : 0x7fffffff;
       const bool live = __any_sync(0xffffffffu, valid);
       const int ctx = s.past + s.n;
       const int v_end = s.past + (t0 + tok < s.n ? t0 + tok : s.n);
       float m = -INFINITY;
       float2 l = make_float2(0.f, 0.f);
+#pragma unroll 1
       for (int i = 0; i < mine; ++i, ++n) {
-        const int j = s.j0 + i, b = (turn + 2 * i + 1) % ST, use = (turn + 2 * i + 1) / ST;
+        const int j = s.j0 + i;
+        ptx::mbar_wait_warp(&s_full[t], n & 1, dead);
+        ptx::tc_fence_after();
         if ((j + 1) * CTC_KB > ctx) {
-          // values behind the request's last key, as far as the product reads: zeros
+          // values behind the request's last key, as far as the product reads: zeros, from both tiles' warps.  (S of this block has been issued
+          // behind products of the block two before at least: the V tiles up to that one have landed, and the phase waited for is the
+          // next one of its barrier.)
           const int first = ctx - j * CTC_KB;
           if (row >= first && row < ((first + 15) & ~15)) {
-            ptx::mbar_wait_lanes(&kv_full[b], use & 1, dead);
-            uint4* v = reinterpret_cast<uint4*>(sKV + b * Sh::TILE + row * 128);
+            const int b = (gb + i) % VS;
+            ptx::mbar_wait_lanes(&v_full[b], ((gb + i) / VS) & 1, dead);
+            uint4* v = reinterpret_cast<uint4*>(sV + b * Sh::TILE + row * 128);
 #pragma unroll
             for (int h = 0; h < Sh::NC; ++h)
 #pragma unroll
@@ -480,19 +593,20 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           }
           __syncwarp();
         }
-        ptx::mbar_wait_warp(&s_full[t], n & 1, dead);
-        ptx::tc_fence_after();
+        SOD2_TRACE(t, 100 + n)
         if (live) {
           uint32_t sc[128];
 #pragma unroll
           for (int h = 0; h < 4; ++h) ptx::tmem_ld32(tS + h * 32, sc + h * 32);
           ptx::tmem_ld_wait();
+          SOD2_TRACE(t, 200 + n)
           const int seen = lim - j * CTC_KB;
           if (__any_sync(0xffffffffu, seen < CTC_KB)) {
 #pragma unroll
             for (int e = 0; e < 128; ++e) if (e >= seen) sc[e] = 0xff800000u;   // -inf
           }
-          const float mx = ctc_max32(ctc_max32(ctc_max32(ctc_max32(-INFINITY, sc), sc + 32), sc + 64), sc + 96);
+          const float mx = ctc_max128(sc);
+          SOD2_TRACE(t, 300 + n)
           const bool move = (mx - m) * c > 8.0f;            // false while both are -inf
           if (i == 0) m = mx;
           else if (__any_sync(0xffffffffu, move)) {
@@ -510,7 +624,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;       // a row that has seen nothing: all its P are zero
-          const float2 c2 = make_float2(c, c), mc2 = make_float2(-ref * c, -ref * c);
+          const float2 c2 = make_float2(c, c), mc2 = make_float2(fmaf(-ref, c, CtcType<T>::shift), fmaf(-ref, c, CtcType<T>::shift));
           const int upto = v_end - j * CTC_KB;              // columns that the product reads
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
@@ -519,14 +633,23 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
               ctc_exp32<T>(sc + h * 32, pk, c2, mc2, &l);
               ptx::tmem_st16(tS + h * 16, pk);
             }
+            if (h == 1) {
+              ptx::tmem_st_wait();
+              ptx::tc_fence_before();
+              __syncwarp();
+              ptx::mbar_arrive_warp(&p_half[t]);
+            }
           }
           ptx::tmem_st_wait();
+        } else {
+          ptx::mbar_arrive_warp(&p_half[t]);
         }
         ptx::tc_fence_before();
         __syncwarp();
         ptx::mbar_arrive_warp(&p_full[t]);
+        SOD2_TRACE(t, 400 + n)
       }
-      turn += 2 * len;
+      gb += len;
       // ---- the segment's end
       if (mine > 0) { ptx::mbar_wait_warp(&o_full[t], (n - 1) & 1, dead); ptx::tc_fence_after(); }
       const float lsum = l.x + l.y;
@@ -566,7 +689,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           const int src = __ffs(redo) - 1;
           redo &= redo - 1;
           const int rr = __shfl_sync(0xffffffffu, static_cast<int>(orow), src), hh = __shfl_sync(0xffffffffu, h, src), seen = __shfl_sync(0xffffffffu, lim, src);
-          causal_row<T>(p.c, s.r, s.first, rr, hh, seen);
+          causal_row<T>(p.c, s.r, s.first, rr, hh, seen, 0, 1);
         }
       } else {
         const long long tile = (2LL * blockIdx.x + (s.starts ? 1 : 0)) * 2 + t;
@@ -644,7 +767,7 @@ __global__ void __launch_bounds__(256) causal_join(const __grid_constant__ CtcPa
     const int rr = (blockIdx.y & 3) * 32 + r, tt = rr / p.G;
     if (tt >= p.tok || t0 + tt >= q.n) continue;
     const int h = d.z * p.G + rr - tt * p.G, orow = q.first + t0 + tt;
-    if (odd_s[r]) { causal_row<T>(p.c, d.y, q.first, orow, h, q.past + t0 + tt + 1); continue; }
+    if (odd_s[r]) { causal_row<T>(p.c, d.y, q.first, orow, h, q.past + t0 + tt + 1, 0, 1); continue; }
     T* o = static_cast<T*>(p.c.o) + orow * p.c.o_ts + h * p.c.o_hs;
     for (int e = lane; e < p.c.D; e += 32) o[e] = rope_store<T>(out_s[r][e]);
   }
