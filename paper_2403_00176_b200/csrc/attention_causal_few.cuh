@@ -1,0 +1,384 @@
+// Attention over a paged cache for few query rows: single tokens, short drafts.  (attention_causal.cuh has the definition.)
+//
+// Every key and value of a request is read once for up to 16 query rows (tokens x heads of one key head), so reading them is all the
+// time there is: the kernel is a stream of the cache through shared memory.  An item is 16 query rows of a request and key head; the CTAs
+// (one per SM) share the items' blocks evenly, as attention_causal_division.cuh describes, and causal_few_join puts cut items together.
+// With 16 rows a tcgen05.mma would leave seven eighths of its 128 rows empty and the scores in one warp's quarter of TMEM, so the products are
+// mma.sync m16n8k16: 2 x 64 of them a block of 128 keys and head size 128, an eighth of it per warp, beside 64 KB of loads.
+//   warps 0..7  16 of the block's 128 keys each: S = Q K^T (16 x 16), P = 2^(S c - m), O += P V, with a maximum, sum and O of their own in
+//               registers; no exchange until the item ends, where the eight are put together through shared memory
+//   warp 8 / 9  load K / V: a box per page and 64 columns, lanes side by side
+// Maximum, sum and O are 32-bit, P is rounded once to the type of the values.  The exponent reference moves only when a score exceeds it by
+// more than 2^8, so a block needs no shuffles but then.  Keys behind a row's last are masked by selection, values behind the request's
+// last key zeroed in shared memory; a row whose result is not finite is computed again key by key (causal_row).
+#pragma once
+#include <cuda.h>
+#include "attention_causal_division.cuh"
+#include "ptx.cuh"
+
+namespace sod2 {
+namespace k {
+
+constexpr int CFW_ROWS = 16, CFW_KB = 128, CFW_WARPS = 8, CFW_THREADS = (CFW_WARPS + 2) * 32, CFW_GRID = 148;
+
+struct CfwParams {
+  static constexpr int KB = CFW_KB, START = 1, SNAP = 2, THREADS = CFW_THREADS;
+  __device__ __forceinline__ int items(const CausalReq& q) const { return static_cast<int>((static_cast<long long>(q.n) * G + CFW_ROWS - 1) / CFW_ROWS); }
+  __device__ __forceinline__ int end(int idx) const { return static_cast<int>((static_cast<long long>(idx) * CFW_ROWS + CFW_ROWS - 1) / G) + 1; }
+  __device__ __forceinline__ bool takes(int n) const { return n <= most; }
+  CausalParams c;
+  float scale_log2e;
+  int G, ksteps, box_rows, cut;
+  int most;                   // requests of more new tokens are another kernel's
+  float* part_o;              // [2 * CFW_GRID slots][16 rows][DP]
+  float2* part_ml;            // [2 * CFW_GRID slots][16]: reference (log2) and sum
+  int4* desc;                 // [2 * CFW_GRID], as CtcParams::desc
+};
+
+template <int DP> struct CfwShape {
+  static constexpr int NC = DP / 64, CHUNK = CFW_KB * 128, TILE = NC * CHUNK;      // K or V of a block
+  static constexpr int ST = DP == 128 ? 3 : 6;                                     // blocks in flight: 192 KB
+  static constexpr int JOIN = CFW_WARPS * 8 * DP * 4;                              // eight rows of every warp's O
+  static constexpr int SMEM = 2 * ST * TILE + JOIN + CFW_WARPS * CFW_ROWS * 8 + 256 + 64;
+};
+
+template <class T> struct CfwType;
+template <> struct CfwType<__nv_bfloat16> {
+  static constexpr float shift = 0.f;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
+  static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <> struct CfwType<__half> {
+  static constexpr float shift = 7.f;       // a factor 2^7 on P, its sum and O: see attention_causal_tcgen05.cuh
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
+  static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+__device__ __forceinline__ void cfw_ldsm(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void cfw_ldsm_t(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float cfw_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// all consumer warps
+__device__ __forceinline__ void cfw_sync() { asm volatile("bar.sync 1, %0;" ::"n"(CFW_WARPS * 32) : "memory"); }
+
+template <class T, int DP>
+__global__ void __launch_bounds__(CFW_THREADS, 1)
+causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CfwParams p) {
+  using Sh = CfwShape<DP>;
+  constexpr int ST = Sh::ST;
+  extern __shared__ __align__(1024) uint8_t cfw_smem[];
+  uint8_t* sK = cfw_smem;                                               // [ST]
+  uint8_t* sV = sK + ST * Sh::TILE;                                     // [ST]
+  float* o_s = reinterpret_cast<float*>(sV + ST * Sh::TILE);            // [8 warps][8 rows][DP]
+  float2* ml_s = reinterpret_cast<float2*>(o_s + CFW_WARPS * 8 * DP);   // [8 warps][16 rows] reference and sum
+  uint64_t* bars = reinterpret_cast<uint64_t*>(ml_s + CFW_WARPS * CFW_ROWS);
+  uint64_t* k_full = bars;            // [ST]
+  uint64_t* v_full = bars + ST;       // [ST]
+  uint64_t* freed = bars + 2 * ST;    // [ST] all consumers are through with both
+  volatile int* dead = reinterpret_cast<volatile int*>(bars + 3 * ST);
+  CausalSpot* spot = reinterpret_cast<CausalSpot*>(bars + 3 * ST + 1);  // [2]
+  static_assert((3 * ST + 1) * 8 + 2 * sizeof(CausalSpot) <= 256 + 64, "");
+  long long* weight = reinterpret_cast<long long*>(sK);                 // [CFW_THREADS], ahead of the first load
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < ST; ++b) { ptx::mbar_init(&k_full[b], 1); ptx::mbar_init(&v_full[b], 1); ptx::mbar_init(&freed[b], CFW_WARPS); }
+    *dead = 0;
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmK);
+    ptx::prefetch_tmap(&tmV);
+  }
+  causal_divide(p, weight, spot);
+  ptx::fence_proxy_async();           // the division's scratch becomes the load ring
+  __syncthreads();
+  const CausalSpot from = spot[0], to = spot[1];
+  const long long units = to.at - from.at;
+  ptx::pdl_launch();
+  if (p.cut && threadIdx.x < 2) {     // what this CTA leaves in its two slots
+    int4 d = make_int4(0, 0, 0, 0);
+    if (threadIdx.x == 0) {           // the item that an earlier CTA began
+      if (from.off > 0 && units > 0) d = make_int4(to.off > 0 && to.item == from.item ? 1 : 2, from.r, from.head, from.idx);
+    } else if (to.off > 0 && to.item >= from.at) {                  // the item that this CTA begins and leaves unfinished
+      d = make_int4(1, to.r, to.head, to.idx);
+    }
+    p.desc[2 * blockIdx.x + threadIdx.x] = d;
+  }
+  CausalWalk<CfwParams> walk;
+  walk.start(p, from, units);
+  CausalSeg s;
+  int stage = 0, use = 0;
+
+  if (warp >= CFW_WARPS) {
+    // ---- producers
+    const bool is_k = warp == CFW_WARPS;
+    const CUtensorMap* tm = is_k ? &tmK : &tmV;
+    uint64_t* full = is_k ? k_full : v_full;
+    uint8_t* ring = is_k ? sK : sV;
+    const int per = CFW_KB / p.box_rows;                  // boxes of 64 columns in a block
+    const int chunk = lane / per, box = lane - chunk * per;
+    int bad = 0;
+#pragma unroll 1
+    while (walk.next(p, s)) {
+      const int ctx = s.past + s.n;
+      const int* ids = p.c.table + s.r * p.c.table_stride;
+      // the page of this lane's box, looked up a block ahead
+      auto page_of = [&](int j) {
+        const int row = j * CFW_KB + box * p.box_rows;
+        return chunk < Sh::NC && j < s.j1 && row < ctx ? ids[row / p.c.page] : 0;
+      };
+      int id = page_of(s.j0);
+#pragma unroll 1
+      for (int j = s.j0; j < s.j1; ++j) {
+        const int row = j * CFW_KB + box * p.box_rows;
+        const bool mine = chunk < Sh::NC && row < ctx;
+        const int ahead = page_of(j + 1);
+        if (use > 0) ptx::mbar_wait_warp(&freed[stage], (use - 1) & 1, dead);
+        const int n = __popc(__ballot_sync(0xffffffffu, mine));
+        if (!*dead) {
+          if (lane == 0) ptx::mbar_expect_tx(&full[stage], n * p.box_rows * 128);
+          __syncwarp();
+          if (mine) {
+            int page = id;
+            if (page < 0 || page >= p.c.n_pages) { page = p.c.n_pages; bad = SERVE_BAD_PAGE; }     // outside the map: zeros
+            ptx::tma_load_4d(ring + stage * Sh::TILE + chunk * Sh::CHUNK + box * p.box_rows * 128, tm, chunk * 64, row % p.c.page, s.head, page, &full[stage]);
+          }
+        }
+        __syncwarp();
+        id = ahead;
+        if (++stage == ST) { stage = 0; ++use; }
+      }
+    }
+    if (bad && p.c.status) atomicOr(p.c.status, bad);
+  } else {
+    // ---- consumers: keys 16 warp .. 16 warp + 15 of every block
+    const float c = p.scale_log2e;
+    const int r0 = lane >> 2, col = (lane & 3) * 2;       // rows r0 and r0 + 8, columns col, col + 1 of each 8
+    // places of ldmatrix: of K the keys are matrix columns, of V (transposed) matrix rows
+    const int k_key = warp * 16 + (lane & 7) + ((lane >> 4) << 3), k_unit = (lane >> 3) & 1;
+    const int v_key = warp * 16 + (lane & 15), v_unit = lane >> 4;
+    const uint32_t k_base = ptx::smem_u32(sK) + k_key * 128, v_base = ptx::smem_u32(sV) + v_key * 128;
+#pragma unroll 1
+    while (walk.next(p, s)) {
+      const int ctx = s.past + s.n, row0 = s.idx * CFW_ROWS, rows = s.n * p.G - row0;      // rows of the item: min(rows, 16)
+      // per row: its token, the keys it sees
+      int lim[2];
+      uint32_t q[DP / 16][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = row0 + r0 + h * 8, t = r / p.G, g = r - t * p.G;
+        const bool valid = r0 + h * 8 < rows;
+        lim[h] = valid ? s.past + t + 1 : 0x7fffffff;       // rows that are not there: unmasked, never stored
+        const T* src = static_cast<const T*>(p.c.q) + (s.first + (valid ? t : 0)) * p.c.q_ts + (s.head * p.G + (valid ? g : 0)) * p.c.q_hs;
+#pragma unroll
+        for (int kk = 0; kk < DP / 16; ++kk)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int d = kk * 16 + e * 8 + col;
+            q[kk][h + 2 * e] = valid && d < p.c.D ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
+          }
+      }
+      const int least = s.past + row0 / p.G + 1;            // keys that the item's first row sees
+      float o[DP / 8][4];
+#pragma unroll
+      for (int e = 0; e < DP / 8; ++e) { o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f; }
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll 1
+      for (int j = s.j0; j < s.j1; ++j) {
+        const int key0 = j * CFW_KB + warp * 16;
+        ptx::mbar_wait_warp(&k_full[stage], use & 1, dead);
+        if (key0 < ctx) {
+          float sc[2][4] = {};
+          const uint32_t ka = k_base + stage * Sh::TILE;
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk) {
+            if (kk < p.ksteps) {
+              uint32_t b[4];
+              cfw_ldsm(b, ka + (kk >> 2) * Sh::CHUNK + (((2 * (kk & 3) + k_unit) ^ (k_key & 7)) << 4));
+              CfwType<T>::mma(sc[0], q[kk], b[0], b[1]);
+              CfwType<T>::mma(sc[1], q[kk], b[2], b[3]);
+            }
+          }
+          if (key0 + 16 > least) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int key = key0 + (e >> 2) * 8 + col + (e & 1);
+              if (key >= lim[(e >> 1) & 1] || key >= ctx) sc[e >> 2][e & 3] = -INFINITY;
+            }
+          }
+          float mx[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(sc[0][2 * h], sc[0][2 * h + 1]), fmaxf(sc[1][2 * h], sc[1][2 * h + 1]));
+          // (m = -inf and a finite maximum: moves; both -inf: does not)
+          if (__any_sync(0xffffffffu, (mx[0] - m[0]) * c > 8.f || (mx[1] - m[1]) * c > 8.f)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
+              mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+              const float now = fmaxf(m[h], mx[h]), corr = now == m[h] ? 1.f : cfw_ex2((m[h] - now) * c);
+              m[h] = now;
+              l[h] *= corr;
+#pragma unroll
+              for (int e = 0; e < DP / 8; ++e) { o[e][2 * h] *= corr; o[e][2 * h + 1] *= corr; }
+            }
+          }
+          uint32_t pa[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float mc = m[h] == -INFINITY ? 0.f : fmaf(-m[h], c, CfwType<T>::shift);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const float x = cfw_ex2(fmaf(sc[t][2 * h], c, mc)), y = cfw_ex2(fmaf(sc[t][2 * h + 1], c, mc));
+              l[h] += x + y;
+              pa[h + 2 * t] = CfwType<T>::pack(x, y);
+            }
+          }
+          ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
+          if (key0 + 16 > ctx) {
+            // values behind the request's last key: zeros
+            const int key = lane >> 1;
+            if (key0 + key >= ctx) {
+              uint4* v = reinterpret_cast<uint4*>(sV + stage * Sh::TILE + (warp * 16 + key) * 128) + (lane & 1) * 4;
+#pragma unroll
+              for (int h = 0; h < Sh::NC; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[h * (Sh::CHUNK / 16) + e] = make_uint4(0, 0, 0, 0);
+              ptx::fence_proxy_async();
+            }
+            __syncwarp();
+          }
+          const uint32_t va = v_base + stage * Sh::TILE;
+#pragma unroll
+          for (int dt = 0; dt < DP / 16; ++dt) {
+            if (dt < p.ksteps) {
+              uint32_t b[4];
+              cfw_ldsm_t(b, va + (dt >> 2) * Sh::CHUNK + (((2 * (dt & 3) + v_unit) ^ (v_key & 7)) << 4));
+              CfwType<T>::mma(o[2 * dt], pa, b[0], b[1]);
+              CfwType<T>::mma(o[2 * dt + 1], pa, b[2], b[3]);
+            }
+          }
+        } else {
+          ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
+        }
+        __syncwarp();
+        ptx::mbar_arrive_warp(&freed[stage]);
+        if (++stage == ST) { stage = 0; ++use; }
+      }
+      // ---- the item's end: the eight warps' parts, eight rows at a time; warp w then has row w
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        if ((lane & 3) == 0) ml_s[warp * CFW_ROWS + r0 + h * 8] = make_float2(m[h], l[h]);
+      }
+      const bool whole = s.starts && s.ends;
+      const long long slot = 2LL * blockIdx.x + (s.starts ? 1 : 0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h * 8 >= rows) break;
+        // columns are stored with their eights exchanged by the row: four rows of a column lie in different banks
+#pragma unroll
+        for (int e = 0; e < DP / 8; ++e)
+          *reinterpret_cast<float2*>(o_s + (warp * 8 + r0) * DP + ((e * 8) ^ ((r0 & 3) << 3)) + col) = make_float2(o[e][2 * h], o[e][2 * h + 1]);
+        cfw_sync();
+        const int r = h * 8 + warp;
+        if (r < rows) {
+          float top = -INFINITY, sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < CFW_WARPS; ++w) top = fmaxf(top, ml_s[w * CFW_ROWS + r].x);
+          constexpr int PER = DP / 32;
+          float acc[PER] = {};
+#pragma unroll
+          for (int w = 0; w < CFW_WARPS; ++w) {
+            const float2 ml = ml_s[w * CFW_ROWS + r];
+            const float f = ml.x == -INFINITY ? 0.f : cfw_ex2((ml.x - top) * c);
+            if (ml.x != -INFINITY) {                        // (a warp whose keys the row did not see; NaN goes on)
+              sum = fmaf(f, ml.y, sum);
+              const float* src = o_s + (w * 8 + warp) * DP + ((lane * PER) ^ ((warp & 3) << 3));
+#pragma unroll
+              for (int e = 0; e < PER; ++e) acc[e] = fmaf(f, src[e], acc[e]);
+            }
+          }
+          const int rr = row0 + r, t = rr / p.G, head = s.head * p.G + rr - t * p.G, seen = s.past + t + 1;
+          if (whole) {
+            const float inv = seen > 0 ? 1.f / sum : 0.f;
+            T* dst = static_cast<T*>(p.c.o) + (s.first + t) * p.c.o_ts + head * p.c.o_hs;
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) { acc[e] *= inv; odd |= !(fabsf(acc[e]) < INFINITY); }
+            odd = odd && lane * PER < p.c.D;
+            if (__any_sync(0xffffffffu, odd)) {
+              causal_row<T>(p.c, s.r, s.first, s.first + t, head, seen, 0, 1);
+            } else if (lane * PER < p.c.D) {
+#pragma unroll
+              for (int e = 0; e < PER; e += 2) *reinterpret_cast<uint32_t*>(dst + lane * PER + e) = CfwType<T>::pack(acc[e], acc[e + 1]);
+            }
+          } else {
+            float* po = p.part_o + (slot * CFW_ROWS + r) * DP + lane * PER;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) po[e] = acc[e];
+            if (lane == 0) p.part_ml[slot * CFW_ROWS + r] = make_float2(top == -INFINITY ? -INFINITY : top * c, sum);
+          }
+        }
+        cfw_sync();
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && *dead && p.c.status) atomicOr(p.c.status, 1);
+}
+
+// Puts the parts of a cut item together: CTA c the item that CTA c of the attention began and left unfinished, if any; a warp per row,
+// parts in their order.
+template <class T, int DP>
+__global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_constant__ CfwParams p) {
+  const int c = blockIdx.x, r = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ptx::pdl_wait();
+  const int4 d = p.desc[2 * c + 1];
+  if (d.x == 0) return;
+  const CausalReq q = causal_request(p, d.y);
+  const int rr = d.w * CFW_ROWS + r, t = rr / p.G;
+  if (t >= q.n) return;
+  int last = c;                       // the CTA that ends the item
+  while (last + 1 < CFW_GRID) { ++last; if (p.desc[2 * last].x == 2) break; }
+  auto slot_of = [&](int i) { return 2LL * i + (i == c ? 1 : 0); };
+  float m = -INFINITY;
+  for (int i = c; i <= last; ++i) if (i == c || p.desc[2 * i].x) m = fmaxf(m, p.part_ml[slot_of(i) * CFW_ROWS + r].x);
+  constexpr int PER = DP / 32;
+  float l = 0.f, acc[PER] = {};
+  for (int i = c; i <= last; ++i) {
+    if (i != c && !p.desc[2 * i].x) continue;
+    const float2 ml = p.part_ml[slot_of(i) * CFW_ROWS + r];
+    if (ml.x == -INFINITY) continue;  // a part in which the row saw nothing
+    const float w = exp2f(ml.x - m);
+    l = fmaf(w, ml.y, l);
+    const float* po = p.part_o + (slot_of(i) * CFW_ROWS + r) * DP + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = fmaf(w, po[e], acc[e]);
+  }
+  const int seen = q.past + t + 1, head = d.z * p.G + rr - t * p.G;
+  const float inv = seen > 0 ? 1.f / l : 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) { acc[e] *= inv; odd |= !(fabsf(acc[e]) < INFINITY); }
+  odd = odd && lane * PER < p.c.D;
+  if (__any_sync(0xffffffffu, odd)) { causal_row<T>(p.c, d.y, q.first, q.first + t, head, seen, 0, 1); return; }
+  T* dst = static_cast<T*>(p.c.o) + (q.first + t) * p.c.o_ts + head * p.c.o_hs;
+  if (lane * PER < p.c.D)
+#pragma unroll
+    for (int e = 0; e < PER; e += 2) *reinterpret_cast<uint32_t*>(dst + lane * PER + e) = CfwType<T>::pack(acc[e], acc[e + 1]);
+}
+
+}  // namespace k
+}  // namespace sod2

@@ -35,7 +35,7 @@
 #pragma once
 #include <cuda.h>
 #include <type_traits>
-#include "attention_causal.cuh"
+#include "attention_causal_division.cuh"
 #include "ptx.cuh"
 
 namespace sod2 {
@@ -45,18 +45,22 @@ constexpr int CTC_THREADS = 384;
 constexpr int CTC_GRID = 148;              // CTAs of the division: one per SM
 constexpr int CTC_KB = 128;                // keys per block
 constexpr int CTC_CHUNK = 128 * 128;       // bytes of 128 rows x 64 elements
-constexpr int CTC_PLAN = CTC_THREADS;      // requests per step of the division
 constexpr int CTC_START = 3;               // weight of an item's start and end, in blocks (1: 908, 2: 1015, 3: 1034 TFLOP/s at 8192 tokens; the first
                                            // items of a head are the shortest, and their CTAs end last where it is too low)
 constexpr int CTC_SNAP = 2;                // blocks: cuts closer than this to an item's ends move there
 
 struct CtcParams {
+  static constexpr int KB = CTC_KB, START = CTC_START, SNAP = CTC_SNAP, THREADS = CTC_THREADS;
+  __device__ __forceinline__ int items(const CausalReq& q) const { return (q.n + 2 * tok - 1) / (2 * tok); }
+  __device__ __forceinline__ int end(int idx) const { return (idx + 1) * 2 * tok; }
+  __device__ __forceinline__ bool takes(int n) const { return n > past_rows; }
   CausalParams c;
   float scale_log2e;
   int G, tok;                 // heads per key head, tokens per tile
   int ksteps, n_pv;           // head size in steps of 16, and rounded up to 16
   int box_rows;               // keys per TMA box
   int cut;                    // 1: items may be cut (the workspace is there)
+  int past_rows;              // requests of up to this many new tokens are another kernel's
   float* part_o;              // [2 * CTC_GRID slots][2 tiles][DP][128 rows]
   float2* part_ml;            // [2 * CTC_GRID slots][2 tiles][128 rows]: reference (log2) and sum
   int4* desc;                 // [2 * CTC_GRID]: state (0 none, 1 part, 2 part that ends the item), request, key head, item of the head
@@ -69,178 +73,6 @@ template <int DP> struct CtcShape {
   static constexpr int SMEM = (2 + KS + VS) * TILE + 512 /*barriers, division*/;
   static constexpr uint32_t TM_S = 0, TM_O = 256;       // columns: S (and P) at 128 per tile, O at DP per tile
 };
-
-// ------------------------------------------------------------------------------------------------ division of the work
-struct CtcReq { int first, n, past; };     // n = 0: nothing to do
-__device__ __forceinline__ CtcReq ctc_request(const CausalParams& c, int r) {
-  CtcReq q;
-  q.first = causal_cu(c, r);
-  const int n = causal_cu(c, r + 1) - q.first;
-  q.n = n > 0 ? n : 0;
-  q.past = causal_ctx(c, r, q.n) - q.n;    // may be negative: the first rows see nothing
-  return q;
-}
-// blocks of keys that the tokens below `end` see
-__device__ __forceinline__ int ctc_blocks(const CtcReq& q, int end) {
-  const int v = q.past + (end < q.n ? end : q.n);
-  return v > 0 ? (v + CTC_KB - 1) / CTC_KB : 0;
-}
-__device__ __forceinline__ int ctc_items(const CtcReq& q, int tok) { return (q.n + 2 * tok - 1) / (2 * tok); }
-
-struct CtcSpot { long long at, item; int r, head, idx, off; };    // position, its item's first, and where that is
-
-// Moves a position inside an item to where it may be cut.  off: 0 the item's start, else blocks ahead of the cut + CTC_START.
-__device__ __forceinline__ int ctc_snap(int off, int blocks, bool cut) {
-  const int w = blocks + CTC_START, j = off - CTC_START;
-  if (off == 0) return 0;
-  if (!cut || blocks < 2 * CTC_SNAP) return 2 * off <= w ? 0 : w;
-  if (j < CTC_SNAP) return 0;
-  return blocks - j < CTC_SNAP ? w : off;
-}
-
-// A role's walk over the CTA's share.
-struct CtcSeg { int r, head, idx, first, n, past, j0, j1; bool starts, ends; };
-struct CtcWalk {
-  long long left;
-  int r, head, idx, off;
-  CtcReq q;
-  __device__ __forceinline__ void start(const CtcParams& p, const CtcSpot& a, long long units) {
-    left = units; r = a.r; head = a.head; idx = a.idx; off = a.off;
-    q.n = 0;
-    if (left > 0) q = ctc_request(p.c, r);
-  }
-  __device__ __forceinline__ bool next(const CtcParams& p, CtcSeg& s) {
-    if (left <= 0) return false;
-    while (idx >= ctc_items(q, p.tok)) {
-      idx = 0;
-      if (q.n > 0 && ++head < p.c.HK) continue;
-      head = 0;
-      if (++r >= p.c.n_req) { left = 0; return false; }
-      q = ctc_request(p.c, r);
-    }
-    const int blocks = ctc_blocks(q, (idx + 1) * 2 * p.tok), w = blocks + CTC_START;
-    const int end = left < w - off ? off + static_cast<int>(left) : w;
-    s.r = r; s.head = head; s.idx = idx; s.first = q.first; s.n = q.n; s.past = q.past;
-    s.j0 = off > 0 ? off - CTC_START : 0;
-    s.j1 = end - CTC_START;
-    s.starts = off == 0; s.ends = end == w;
-    left -= end - off;
-    off = 0;
-    ++idx;
-    return true;
-  }
-};
-
-// Finds the item that holds position x of a request whose items start at `start`; a whole warp.
-__device__ __forceinline__ CtcSpot ctc_locate(const CtcParams& p, int r, long long start, long long x, bool cut) {
-  const int lane = threadIdx.x & 31;
-  const CtcReq q = ctc_request(p.c, r);
-  const int np = ctc_items(q, p.tok);
-  long long per = 0;                      // weight of one key head
-#pragma unroll 1
-  for (int i = lane; i < np; i += 32) per += ctc_blocks(q, (i + 1) * 2 * p.tok) + CTC_START;
-#pragma unroll
-  for (int d = 16; d; d >>= 1) per += __shfl_xor_sync(0xffffffffu, per, d);
-  CtcSpot s;
-  s.r = r; s.at = x;
-  s.head = per > 0 ? static_cast<int>((x - start) / per) : 0;
-  long long base = start + s.head * per;
-#pragma unroll 1
-  for (int i0 = 0; i0 < np; i0 += 32) {
-    const int w = i0 + lane < np ? ctc_blocks(q, (i0 + lane + 1) * 2 * p.tok) + CTC_START : 0;
-    int inc = w;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(0xffffffffu, inc, d); if (lane >= d) inc += y; }
-    const unsigned hit = __ballot_sync(0xffffffffu, x < base + inc);
-    if (hit) {
-      const int l = __ffs(hit) - 1, wl = __shfl_sync(0xffffffffu, w, l), il = __shfl_sync(0xffffffffu, inc, l);
-      s.idx = i0 + l;
-      s.item = base + il - wl;
-      const int off = ctc_snap(static_cast<int>(x - s.item), wl - CTC_START, cut);
-      s.at = s.item + off;
-      s.off = off;
-      if (off == wl) { s.item = s.at; s.off = 0; ++s.idx; }     // the next item's start; CtcWalk goes on to the next head or request
-      return s;
-    }
-    base += __shfl_sync(0xffffffffu, inc, 31);
-  }
-  s.idx = np; s.item = s.at; s.off = 0;
-  return s;
-}
-
-// The CTA's share: from spot[0] to spot[1].  Called by all threads; `weight` and `spot` are shared.
-__device__ __forceinline__ void ctc_divide(const CtcParams& p, long long* weight, CtcSpot* spot) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  long long total = 0, lo = 0, hi = 0;
-  // once for the total, once more for the places of the share's ends (the same chunk, with few requests)
-#pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
-    long long base = 0;
-#pragma unroll 1
-    for (int r0 = 0; r0 < p.c.n_req; r0 += CTC_PLAN) {
-      const int nr = p.c.n_req - r0 < CTC_PLAN ? p.c.n_req - r0 : CTC_PLAN;
-      if (pass == 0 || p.c.n_req > CTC_PLAN) {
-        __syncthreads();
-        if (static_cast<int>(threadIdx.x) < nr) {
-          const CtcReq q = ctc_request(p.c, r0 + threadIdx.x);
-          const int np = ctc_items(q, p.tok);
-          long long w = 0;
-          if (np <= 64)
-#pragma unroll 1
-            for (int i = 0; i < np; ++i) w += ctc_blocks(q, (i + 1) * 2 * p.tok) + CTC_START;
-          weight[threadIdx.x] = np <= 64 ? w * p.c.HK : -1;
-        }
-        __syncthreads();
-        for (int i = warp; i < nr; i += CTC_THREADS / 32) {        // long requests: a warp each
-          if (weight[i] >= 0) continue;
-          const CtcReq q = ctc_request(p.c, r0 + i);
-          const int np = ctc_items(q, p.tok);
-          long long w = 0;
-#pragma unroll 1
-          for (int t = lane; t < np; t += 32) w += ctc_blocks(q, (t + 1) * 2 * p.tok) + CTC_START;
-#pragma unroll
-          for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
-          __syncwarp();
-          if (lane == 0) weight[i] = w * p.c.HK;
-        }
-        __syncthreads();
-      }
-      // every warp sums the chunk: 12 requests a lane
-      long long sum = 0;
-#pragma unroll 1
-      for (int e = 0; e < CTC_PLAN / 32; ++e) { const int i = lane * (CTC_PLAN / 32) + e; if (i < nr) sum += weight[i]; }
-      long long inc = sum;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, d); if (lane >= d) inc += y; }
-      const long long chunk = __shfl_sync(0xffffffffu, inc, 31);
-      if (pass == 1 && warp < 2) {
-        const long long x = warp == 0 ? lo : hi;
-        if (x >= base && x < base + chunk) {
-          const long long mine = base + inc - sum;
-          const unsigned own = __ballot_sync(0xffffffffu, x >= mine && x < mine + sum);
-          const int l = __ffs(own) - 1;
-          long long start = __shfl_sync(0xffffffffu, mine, l);
-          int i = l * (CTC_PLAN / 32);
-          while (x >= start + weight[i]) { start += weight[i]; ++i; }
-          const CtcSpot s = ctc_locate(p, r0 + i, start, x, p.cut);
-          if (lane == 0) spot[warp] = s;
-        }
-      }
-      base += chunk;
-    }
-    if (pass == 0) {
-      total = base;
-      lo = total * blockIdx.x / gridDim.x;
-      hi = total * (blockIdx.x + 1) / gridDim.x;
-      if (threadIdx.x == 0) {
-        spot[0].at = spot[1].at = total; spot[0].off = spot[1].off = 0; spot[0].item = spot[1].item = total;
-        spot[0].r = spot[1].r = p.c.n_req; spot[0].head = spot[1].head = spot[0].idx = spot[1].idx = 0;
-      }
-      __syncthreads();
-    }
-  }
-  __syncthreads();
-}
 
 // ------------------------------------------------------------------------------------------------ the kernel
 template <class T> struct CtcType;
@@ -317,9 +149,9 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   uint64_t* v_free = v_full + VS;     // [VS] both tiles' products are done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_free + VS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  CtcSpot* spot = reinterpret_cast<CtcSpot*>(v_free + VS + 1);          // [2]
-  static_assert((13 + 2 * KS + 2 * VS) * 8 + 2 * sizeof(CtcSpot) <= 512, "");
-  long long* weight = reinterpret_cast<long long*>(sK);                 // [CTC_PLAN], ahead of the first load
+  CausalSpot* spot = reinterpret_cast<CausalSpot*>(v_free + VS + 1);          // [2]
+  static_assert((13 + 2 * KS + 2 * VS) * 8 + 2 * sizeof(CausalSpot) <= 512, "");
+  long long* weight = reinterpret_cast<long long*>(sK);                 // [CTC_THREADS], ahead of the first load
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -337,13 +169,13 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
   if (warp == 10) { ptx::tmem_alloc(tmem_slot, 512); ptx::tmem_relinquish(); }
   ptx::pdl_wait();
-  ctc_divide(p, weight, spot);
+  causal_divide(p, weight, spot);
   ptx::fence_proxy_async();           // the plan's scratch becomes the load ring
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const CtcSpot from = spot[0], to = spot[1];
+  const CausalSpot from = spot[0], to = spot[1];
   const long long units = to.at - from.at;
   ptx::pdl_launch();
   if (p.cut && threadIdx.x < 2) {     // what this CTA leaves in its two slots
@@ -355,16 +187,16 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     }
     p.desc[2 * blockIdx.x + threadIdx.x] = d;
   }
-  CtcWalk walk;
+  CausalWalk<CtcParams> walk;
   walk.start(p, from, units);
-  CtcSeg s;
+  CausalSeg s;
   const int tok = p.tok;
   // blocks of the segment that tile t takes part in
-  auto blocks_of = [&](const CtcSeg& g, int t) {
+  auto blocks_of = [&](const CausalSeg& g, int t) {
     const int t0 = (2 * g.idx + t) * tok;
     if (t0 >= g.n) return 0;
-    const CtcReq q{g.first, g.n, g.past};
-    const int b = ctc_blocks(q, t0 + tok);
+    const CausalReq q{g.first, g.n, g.past};
+    const int b = causal_blocks<CTC_KB>(q, t0 + tok);
     const int e = b < g.j1 ? b : g.j1;
     return e > g.j0 ? e - g.j0 : 0;
   };
@@ -501,7 +333,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (free_v) ptx::mma_commit(one, &v_free[v_stage]);
         if (t) ++n1; else ++n0;
       };
-      auto next = [&](CtcSeg& g) {            // the next segment with blocks
+      auto next = [&](CausalSeg& g) {            // the next segment with blocks
         while (walk.next(p, g)) if (g.j1 > g.j0) return true;
         return false;
       };
@@ -528,7 +360,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       }
 #pragma unroll 1
       while (more) {
-        CtcSeg s2;
+        CausalSeg s2;
         more = next(s2);
         const int then0 = more ? blocks_of(s2, 0) : 0, then1 = more ? blocks_of(s2, 1) : 0;
         const int len = s.j1 - s.j0;
@@ -730,7 +562,7 @@ __global__ void __launch_bounds__(256) causal_join(const __grid_constant__ CtcPa
   ptx::pdl_wait();
   const int4 d = p.desc[2 * c + 1];
   if (d.x == 0) return;
-  const CtcReq q = ctc_request(p.c, d.y);
+  const CausalReq q = causal_request(p, d.y);
   const int t0 = (2 * d.w + t) * p.tok, rt = row / p.G;
   const bool valid = rt < p.tok && t0 + rt < q.n;
   if (threadIdx.x < 32) odd_s[lane] = 0;

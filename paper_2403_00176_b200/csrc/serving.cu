@@ -8,6 +8,7 @@
 
 #include "../../include/sod2.h"
 #include "attention_causal.cuh"
+#include "attention_causal_few.cuh"
 #include "attention_causal_tcgen05.cuh"
 #include "engine.h"
 #include "kernels_paging.cuh"
@@ -118,67 +119,108 @@ void set_common(k::CausalParams& p, const AttnCall& a) {
   p.scale = a.scale;
 }
 
-// Workspace of the tcgen05 form: two slots per CTA for the parts of cut items, then their descriptions.
-size_t part_floats(int dp) { return static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * dp; }
-size_t workspace_need(int dim) {
-  if (dim > 128 || dim % 8) return 256;
-  const int dp = dim <= 64 ? 64 : 128;
-  return part_floats(dp) * 4 + static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * sizeof(float2) + 2 * k::CTC_GRID * sizeof(int4) + 256;
+// Workspace: two slots per CTA for the parts of cut items and their descriptions, first of the few-row form, then of the tcgen05 form.
+struct Parts { size_t desc, ml, o, end; };
+constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+constexpr Parts parts_at(size_t at, size_t slots, size_t rows, size_t dp) {
+  const size_t ml = up256(at + slots * sizeof(int4)), o = up256(ml + slots * rows * sizeof(float2));
+  return Parts{at, ml, o, up256(o + slots * rows * dp * sizeof(float))};
+}
+Parts few_parts(int dp) { return parts_at(0, 2 * k::CFW_GRID, k::CFW_ROWS, dp); }
+Parts tile_parts(int dp) { return parts_at(few_parts(dp).end, 2 * k::CTC_GRID, 2 * 128, dp); }
+int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
+size_t workspace_need(int dim) { return dim > 128 || dim % 8 ? 256 : tile_parts(padded_dim(dim)).end; }
+
+template <class P>
+void set_parts(P& a, const Parts& at, void* ws) {
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  a.desc = reinterpret_cast<int4*>(w + at.desc);
+  a.part_ml = reinterpret_cast<float2*>(w + at.ml);
+  a.part_o = reinterpret_cast<float*>(w + at.o);
 }
 
-template <class T, int DP>
-cudaError_t launch_ctc(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& p, cudaStream_t st) {
-  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
-  if (once != cudaSuccess) return once;
-  k::causal_attention_tcgen05<T, DP><<<k::CTC_GRID, k::CTC_THREADS, k::CtcShape<DP>::SMEM, st>>>(q, kk, v, p);
-  if (!p.cut) return cudaGetLastError();
+// the join of cut items, which may be scheduled while the attention ends
+template <class P>
+cudaError_t launch_join(void (*join)(P), dim3 grid, int threads, const P& a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(k::CTC_GRID, 8);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k::causal_join<T, DP>, p);
+  return cudaLaunchKernelEx(&cfg, join, a);
 }
 
-// max_keys: the host's bound on the keys of a request.  False where the tensor maps cannot express the operands.
-bool tcgen05_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_keys, void* ws, cudaStream_t st) {
-  const bool f16 = dtype == SOD2_DTYPE_F16;
+template <class T, int DP>
+cudaError_t launch_tiles(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& a, cudaStream_t st) {
+  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
+  if (once != cudaSuccess) return once;
+  k::causal_attention_tcgen05<T, DP><<<k::CTC_GRID, k::CTC_THREADS, k::CtcShape<DP>::SMEM, st>>>(q, kk, v, a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess || !a.cut ? e : launch_join(k::causal_join<T, DP>, dim3(k::CTC_GRID, 8), 256, a, st);
+}
+
+template <class T, int DP>
+cudaError_t launch_few(const CUtensorMap& kk, const CUtensorMap& v, const k::CfwParams& a, cudaStream_t st) {
+  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_few<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CfwShape<DP>::SMEM);
+  if (once != cudaSuccess) return once;
+  k::causal_attention_few<T, DP><<<k::CFW_GRID, k::CFW_THREADS, k::CfwShape<DP>::SMEM, st>>>(kk, v, a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess || !a.cut ? e : launch_join(k::causal_few_join<T, DP>, dim3(k::CFW_GRID), k::CFW_ROWS * 32, a, st);
+}
+
+// max_new, max_keys: the host's bounds on the new tokens (0: none) and the keys of a request.  False where the tensor maps cannot
+// express the operands.
+bool tensor_core_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st) {
+  const bool f16 = dtype == SOD2_DTYPE_F16, paged = p.ctx != nullptr;
   const int G = p.H / p.HK;
-  auto on16 = [](const void* a) { return reinterpret_cast<uintptr_t>(a) % 16 == 0; };
-  if (dtype == SOD2_DTYPE_F32 || p.D > 128 || p.D % 8 || G > 128 || !on16(p.q) || !on16(p.k) || !on16(p.v) || !on16(p.o)) return false;
+  if (dtype == SOD2_DTYPE_F32 || p.D > 128 || p.D % 8 || G > 128 || !on(p.q, 16) || !on(p.k, 16) || !on(p.v, 16) || !on(p.o, 16)) return false;
   if ((p.o_ts | p.o_hs | p.q_ts | p.q_hs | p.k_ps | p.k_ts | p.k_hs | p.v_ps | p.v_ts | p.v_hs) % 8) return false;
-  if (p.ctx && (p.page % 8 || p.n_pages == 0 || p.width == 0)) return false;
-  k::CtcParams a{};
-  a.c = p;
-  a.scale_log2e = p.scale * 1.4426950408889634f;
-  a.G = G;
-  a.tok = 128 / G;
-  a.ksteps = (p.D + 15) / 16;
-  a.n_pv = a.ksteps * 16;
-  a.box_rows = 128;
-  if (p.ctx) { int r = p.page & -p.page; a.box_rows = r < 128 ? r : 128; }    // the largest power of two that pages and blocks share
-  const int dp = p.D <= 64 ? 64 : 128;
-  a.cut = max_keys > (2 * k::CTC_SNAP - 1) * k::CTC_KB;
-  uint8_t* w = static_cast<uint8_t*>(ws);
-  a.desc = reinterpret_cast<int4*>(w);
-  w += 2 * k::CTC_GRID * sizeof(int4);
-  a.part_ml = reinterpret_cast<float2*>(w);
-  w += static_cast<size_t>(2 * k::CTC_GRID) * 2 * 128 * sizeof(float2);
-  a.part_o = reinterpret_cast<float*>(w);
-  const uint64_t T = p.n_tokens, D = p.D, HK = p.HK;
-  CUtensorMap mq, mk, mv;
-  const uint64_t qe[4] = {D, static_cast<uint64_t>(G), T, HK}, qs[3] = {uint64_t(p.q_hs) * 2, uint64_t(p.q_ts) * 2, uint64_t(p.q_hs) * 2 * G};
-  const uint32_t qb[4] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(a.tok), 1}, kb[4] = {64, static_cast<uint32_t>(a.box_rows), 1, 1};
-  const uint64_t ke[4] = {D, p.ctx ? uint64_t(p.page) : T, HK, p.ctx ? uint64_t(p.n_pages) : 1};
+  if (paged && (p.page % 8 || p.n_pages == 0 || p.width == 0)) return false;
+  const int dp = padded_dim(p.D), ksteps = (p.D + 15) / 16;
+  int box_rows = 128;
+  if (paged) { const int r = p.page & -p.page; box_rows = r < 128 ? r : 128; }    // the largest power of two that pages and blocks share
+  const uint64_t T = p.n_tokens, D = p.D, HK = p.HK, g = G;
+  const uint64_t ke[4] = {D, paged ? uint64_t(p.page) : T, HK, paged ? uint64_t(p.n_pages) : 1};
   const uint64_t ks[3] = {uint64_t(p.k_ts) * 2, uint64_t(p.k_hs) * 2, uint64_t(p.k_ps) * 2}, vs[3] = {uint64_t(p.v_ts) * 2, uint64_t(p.v_hs) * 2, uint64_t(p.v_ps) * 2};
-  if (!encode_16bit_4d(&mq, f16, p.q, qe, qs, qb) || !encode_16bit_4d(&mk, f16, p.k, ke, ks, kb) || !encode_16bit_4d(&mv, f16, p.v, ke, vs, kb)) return false;
-  cudaError_t e;
-  if (f16) e = dp == 64 ? launch_ctc<__half, 64>(mq, mk, mv, a, st) : launch_ctc<__half, 128>(mq, mk, mv, a, st);
-  else e = dp == 64 ? launch_ctc<__nv_bfloat16, 64>(mq, mk, mv, a, st) : launch_ctc<__nv_bfloat16, 128>(mq, mk, mv, a, st);
+  const uint32_t kb[4] = {64, static_cast<uint32_t>(box_rows), 1, 1};
+  CUtensorMap mq, mk, mv;
+  if (!encode_16bit_4d(&mk, f16, p.k, ke, ks, kb) || !encode_16bit_4d(&mv, f16, p.v, ke, vs, kb)) return false;
+  // Over a cache, requests of up to 16 rows (new tokens x heads of a group) take the few-row form.  It takes all requests where the
+  // host's bound says that none has more (one that has more is right there too, and reads its keys once per 16 rows).
+  const int few = paged && G <= k::CFW_ROWS ? k::CFW_ROWS / G : 0;
+  const bool all_few = few > 0 && max_new > 0 && max_new <= few;
+  k::CtcParams a{};
+  if (!all_few) {
+    const uint64_t qe[4] = {D, g, T, HK}, qs[3] = {uint64_t(p.q_hs) * 2, uint64_t(p.q_ts) * 2, uint64_t(p.q_hs) * 2 * g};
+    const uint32_t qb[4] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(128 / G), 1};
+    if (!encode_16bit_4d(&mq, f16, p.q, qe, qs, qb)) return false;
+  }
+  cudaError_t e = cudaSuccess;
+  if (few > 0) {
+    k::CfwParams b{};
+    b.c = p;
+    b.scale_log2e = p.scale * 1.4426950408889634f;
+    b.G = G; b.ksteps = ksteps; b.box_rows = box_rows;
+    b.cut = max_keys > (2 * k::CfwParams::SNAP - 1) * k::CFW_KB;
+    b.most = all_few ? 0x7fffffff : few;
+    set_parts(b, few_parts(dp), ws);
+    if (f16) e = dp == 64 ? launch_few<__half, 64>(mk, mv, b, st) : launch_few<__half, 128>(mk, mv, b, st);
+    else e = dp == 64 ? launch_few<__nv_bfloat16, 64>(mk, mv, b, st) : launch_few<__nv_bfloat16, 128>(mk, mv, b, st);
+  }
+  if (!all_few && e == cudaSuccess) {
+    a.c = p;
+    a.scale_log2e = p.scale * 1.4426950408889634f;
+    a.G = G; a.tok = 128 / G; a.ksteps = ksteps; a.n_pv = ksteps * 16; a.box_rows = box_rows;
+    a.cut = max_keys > (2 * k::CtcParams::SNAP - 1) * k::CTC_KB;
+    a.past_rows = few;
+    set_parts(a, tile_parts(dp), ws);
+    if (f16) e = dp == 64 ? launch_tiles<__half, 64>(mq, mk, mv, a, st) : launch_tiles<__half, 128>(mq, mk, mv, a, st);
+    else e = dp == 64 ? launch_tiles<__nv_bfloat16, 64>(mq, mk, mv, a, st) : launch_tiles<__nv_bfloat16, 128>(mq, mk, mv, a, st);
+  }
   if (e != cudaSuccess) { cudaGetLastError(); c.need(false, SOD2_E_CUDA, cudaGetErrorString(e)); }
   return true;
 }
@@ -189,8 +231,8 @@ void check_workspace(Check& c, int dim, const void* ws, size_t bytes) {
   c.need(on(ws, 256), SOD2_E_MISALIGNED, "workspace must be 256-byte aligned");
 }
 
-void launch_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_keys, void* ws, cudaStream_t st) {
-  if (tcgen05_attention(c, p, dtype, max_keys, ws, st)) return;
+void launch_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st) {
+  if (tensor_core_attention(c, p, dtype, max_new, max_keys, ws, st)) return;
   const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) * p.H + 3) / 4);
   if (dtype == SOD2_DTYPE_F32) k::causal_attention_rows<float><<<grid, 128, 0, st>>>(p);
   else if (dtype == SOD2_DTYPE_F16) k::causal_attention_rows<__half><<<grid, 128, 0, st>>>(p);
@@ -333,7 +375,7 @@ extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t 
     p.k = k->data; p.k_ts = k->token_stride; p.k_hs = k->head_stride;
     p.v = v->data; p.v_ts = v->token_stride; p.v_hs = v->head_stride;
     p.status = dev_status;
-    launch_attention(c, p, dtype, n_tokens, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
+    launch_attention(c, p, dtype, 0, n_tokens, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
     return c.status != SOD2_OK ? c.fail() : c.launched();
   });
 }
@@ -365,7 +407,7 @@ extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n
     p.v = v_cache->data; p.v_ps = v_cache->page_stride; p.v_ts = v_cache->token_stride; p.v_hs = v_cache->head_stride;
     p.ctx = dev_ctx; p.table = dev_table; p.table_stride = table_stride; p.width = static_cast<int>(table_width);
     p.page = page_size; p.n_pages = static_cast<int>(n_pages); p.status = dev_status;
-    launch_attention(c, p, dtype, table_width * page_size, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
+    launch_attention(c, p, dtype, max_new, table_width * page_size, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
     return c.status != SOD2_OK ? c.fail() : c.launched();
   });
 }
