@@ -93,6 +93,8 @@ __device__ __noinline__ void causal_row(const CausalParams& p, int request, int 
 // A warp per row and head.  Every key is read by every row that sees it: simple, not fast.
 template <class T>
 __global__ void __launch_bounds__(128) causal_attention_rows(const __grid_constant__ CausalParams p) {
+  ptx::pdl_launch();
+  ptx::pdl_wait();
   const long long item = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
   const int row = static_cast<int>(item / p.H), h = static_cast<int>(item % p.H);
   if (row >= p.n_tokens || row < causal_cu(p, 0) || row >= causal_cu(p, p.n_req)) return;

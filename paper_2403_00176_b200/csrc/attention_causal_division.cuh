@@ -1,8 +1,9 @@
 // Division of the work of the attention kernels over their CTAs, on the device, where all lengths are.
 // Items (some query rows of one request and key head, all its blocks of keys) are laid end to end in the order request, key head, rows; an
 // item weighs its blocks and START more for its start and end.  CTA b of n takes what lies between b / n and (b + 1) / n of the whole.
-// A parameter block P says what an item is: KB keys a block, START, SNAP (cuts closer than this many blocks to an item's ends move there),
-// THREADS of a CTA, items(q) of a request and head, end(i): the tokens below it see the keys of item i, and takes(n): whether
+// A parameter block P says what an item is: KB keys a block, START, WHOLE (items of fewer blocks are not cut), SNAP
+// (cuts closer than this many blocks to an item's ends move there),
+// THREADS of a CTA, GRID CTAs, items(q) of a request and head, end(i): the tokens below it see the keys of item i, and takes(n): whether
 // requests of n new tokens are this kernel's at all.
 #pragma once
 #include "attention_causal.cuh"
@@ -36,7 +37,7 @@ template <class P>
 __device__ __forceinline__ int causal_snap(int off, int blocks, bool cut) {
   const int w = blocks + P::START, j = off - P::START;
   if (off == 0) return 0;
-  if (!cut || blocks < 2 * P::SNAP) return 2 * off <= w ? 0 : w;
+  if (!cut || blocks < P::WHOLE) return 2 * off <= w ? 0 : w;
   if (j < P::SNAP) return 0;
   return blocks - j < P::SNAP ? w : off;
 }
@@ -75,20 +76,14 @@ struct CausalWalk {
   }
 };
 
-// Finds the item that holds position x of a request whose items start at `start`; a whole warp.
+// Finds the item that holds position x of request r (of whose items `per` is the weight of a key head, the first at `start`); a whole warp.
 template <class P>
-__device__ __forceinline__ CausalSpot causal_locate(const P& p, int r, long long start, long long x, bool cut) {
-  const int lane = threadIdx.x & 31;
-  const CausalReq q = causal_request(p, r);
-  const int np = p.items(q);
-  long long per = 0;                      // weight of one key head
-#pragma unroll 1
-  for (int i = lane; i < np; i += 32) per += causal_item_blocks(p, q, i) + P::START;
-#pragma unroll
-  for (int d = 16; d; d >>= 1) per += __shfl_xor_sync(0xffffffffu, per, d);
+__device__ __forceinline__ CausalSpot causal_locate(const P& p, int r, const CausalReq& q, long long per, long long start, long long x) {
+  const int lane = threadIdx.x & 31, np = p.items(q);
   CausalSpot s;
   s.r = r; s.at = x;
-  s.head = per > 0 ? static_cast<int>((x - start) / per) : 0;
+  const unsigned long long in = static_cast<unsigned long long>(x - start);
+  s.head = static_cast<int>((in | per) >> 32 ? in / static_cast<unsigned long long>(per) : static_cast<unsigned>(in) / static_cast<unsigned>(per));
   long long base = start + s.head * per;
 #pragma unroll 1
   for (int i0 = 0; i0 < np; i0 += 32) {
@@ -101,7 +96,7 @@ __device__ __forceinline__ CausalSpot causal_locate(const P& p, int r, long long
       const int l = __ffs(hit) - 1, wl = __shfl_sync(0xffffffffu, w, l), il = __shfl_sync(0xffffffffu, inc, l);
       s.idx = i0 + l;
       s.item = base + il - wl;
-      const int off = causal_snap<P>(static_cast<int>(x - s.item), wl - P::START, cut);
+      const int off = causal_snap<P>(static_cast<int>(x - s.item), wl - P::START, p.cut);
       s.at = s.item + off;
       s.off = off;
       if (off == wl) { s.item = s.at; s.off = 0; ++s.idx; }     // the next item's start; CausalWalk goes on to the next head or request
@@ -113,79 +108,89 @@ __device__ __forceinline__ CausalSpot causal_locate(const P& p, int r, long long
   return s;
 }
 
-// The CTA's share: from spot[0] to spot[1].  Called by all threads; `weight` and `spot` are shared.
+// The CTA's share: from spot[0] to spot[1].  Called by all threads; `sums` (a value per warp) and `spot` are shared.  A request per thread,
+// THREADS at a time; requests of many items by their whole warp.  One round where the requests are no more than the threads,
+// else one for the total and one for the places.
 template <class P>
-__device__ __forceinline__ void causal_divide(const P& p, long long* weight, CausalSpot* spot) {
+__device__ __forceinline__ void causal_divide(const P& p, long long* sums, CausalSpot* spot) {
+  constexpr int WARPS = P::THREADS / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  long long total = 0, lo = 0, hi = 0;
-  // once for the total, once more for the places of the share's ends (the same chunk, with few requests)
+  const bool many = p.c.n_req > P::THREADS;
+  long long total = 0, base = 0, at[2] = {0, 0};
 #pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
-    long long base = 0;
+  for (int pass = many ? 0 : 1; pass < 2; ++pass) {
+    base = 0;
 #pragma unroll 1
     for (int r0 = 0; r0 < p.c.n_req; r0 += P::THREADS) {
-      const int nr = p.c.n_req - r0 < P::THREADS ? p.c.n_req - r0 : P::THREADS;
-      if (pass == 0 || p.c.n_req > P::THREADS) {
-        __syncthreads();
-        if (static_cast<int>(threadIdx.x) < nr) {
-          const CausalReq q = causal_request(p, r0 + threadIdx.x);
-          const int np = p.items(q);
-          long long w = 0;
-          if (np <= 64)
+      const int r = r0 + threadIdx.x;
+      CausalReq q{0, 0, 0};
+      if (r < p.c.n_req) q = causal_request(p, r);
+      const int np = p.items(q);
+      long long per = 0;              // weight of one key head
+      const bool wide = np > 8;
+      if (!wide)
 #pragma unroll 1
-            for (int i = 0; i < np; ++i) w += causal_item_blocks(p, q, i) + P::START;
-          weight[threadIdx.x] = np <= 64 ? w * p.c.HK : -1;
-        }
-        __syncthreads();
-        for (int i = warp; i < nr; i += P::THREADS / 32) {        // long requests: a warp each
-          if (weight[i] >= 0) continue;
-          const CausalReq q = causal_request(p, r0 + i);
-          const int np = p.items(q);
-          long long w = 0;
+        for (int i = 0; i < np; ++i) per += causal_item_blocks(p, q, i) + P::START;
+      for (unsigned left = __ballot_sync(0xffffffffu, wide); left; left &= left - 1) {
+        const int src = __ffs(left) - 1;
+        const CausalReq w{0, __shfl_sync(0xffffffffu, q.n, src), __shfl_sync(0xffffffffu, q.past, src)};
+        const int nw = p.items(w);
+        long long sum = 0;
 #pragma unroll 1
-          for (int t = lane; t < np; t += 32) w += causal_item_blocks(p, q, t) + P::START;
+        for (int i = lane; i < nw; i += 32) sum += causal_item_blocks(p, w, i) + P::START;
 #pragma unroll
-          for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
-          __syncwarp();
-          if (lane == 0) weight[i] = w * p.c.HK;
-        }
-        __syncthreads();
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == src) per = sum;
       }
-      // every warp sums the chunk: 12 requests a lane
-      long long sum = 0;
-#pragma unroll 1
-      for (int e = 0; e < P::THREADS / 32; ++e) { const int i = lane * (P::THREADS / 32) + e; if (i < nr) sum += weight[i]; }
-      long long inc = sum;
+      const long long w = per * p.c.HK;
+      long long inc = w;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, d); if (lane >= d) inc += y; }
-      const long long chunk = __shfl_sync(0xffffffffu, inc, 31);
-      if (pass == 1 && warp < 2) {
-        const long long x = warp == 0 ? lo : hi;
-        if (x >= base && x < base + chunk) {
-          const long long mine = base + inc - sum;
-          const unsigned own = __ballot_sync(0xffffffffu, x >= mine && x < mine + sum);
-          const int l = __ffs(own) - 1;
-          long long start = __shfl_sync(0xffffffffu, mine, l);
-          int i = l * (P::THREADS / 32);
-          while (x >= start + weight[i]) { start += weight[i]; ++i; }
-          const CausalSpot s = causal_locate(p, r0 + i, start, x, p.cut);
-          if (lane == 0) spot[warp] = s;
+      __syncthreads();                // the sums of the step before have been read
+      if (lane == 31) sums[warp] = inc;
+      __syncthreads();
+      long long start = base + inc - w;
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) {
+        const long long y = sums[i];
+        if (i < warp) start += y;
+        base += y;
+      }
+      if (pass == 1) {
+        if (r0 == 0) {
+          if (!many) total = base;
+          at[0] = static_cast<long long>(static_cast<unsigned long long>(total) * blockIdx.x / P::GRID);
+          at[1] = static_cast<long long>(static_cast<unsigned long long>(total) * (blockIdx.x + 1) / P::GRID);
+        }
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+          const long long x = at[e];
+          const unsigned own = __ballot_sync(0xffffffffu, x >= start && x < start + w);
+          if (own) {
+            const int src = __ffs(own) - 1;
+            const CausalReq o{0, __shfl_sync(0xffffffffu, q.n, src), __shfl_sync(0xffffffffu, q.past, src)};
+            const CausalSpot s = causal_locate(p, r0 + warp * 32 + src, o, __shfl_sync(0xffffffffu, per, src), __shfl_sync(0xffffffffu, start, src), x);
+            if (lane == 0) spot[e] = s;
+          }
         }
       }
-      base += chunk;
     }
-    if (pass == 0) {
-      total = base;
-      lo = total * blockIdx.x / gridDim.x;
-      hi = total * (blockIdx.x + 1) / gridDim.x;
-      if (threadIdx.x == 0) {
-        spot[0].at = spot[1].at = total; spot[0].off = spot[1].off = 0; spot[0].item = spot[1].item = total;
-        spot[0].r = spot[1].r = p.c.n_req; spot[0].head = spot[1].head = spot[0].idx = spot[1].idx = 0;
-      }
-      __syncthreads();
-    }
+    total = base;
   }
+  // a position behind all items
+  if (threadIdx.x < 2 && at[threadIdx.x] >= total) spot[threadIdx.x] = CausalSpot{total, total, p.c.n_req, 0, 0, 0};
   __syncthreads();
+}
+
+// The slots that hold the parts of the item that CTA c began and left unfinished: the last CTA with one.  A whole warp; slots in between may
+// be empty (state 0).
+__device__ __forceinline__ int causal_last_part(const int4* desc, int c, int grid) {
+  const int lane = threadIdx.x & 31;
+  for (int i0 = c + 1; i0 < grid; i0 += 32) {
+    const unsigned end = __ballot_sync(0xffffffffu, i0 + lane < grid && desc[2 * (i0 + lane)].x == 2);
+    if (end) return i0 + __ffs(end) - 1;
+  }
+  return grid - 1;
 }
 
 }  // namespace k

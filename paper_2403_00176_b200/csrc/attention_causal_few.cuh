@@ -22,9 +22,11 @@ namespace k {
 constexpr int CFW_ROWS = 16, CFW_KB = 128, CFW_WARPS = 8, CFW_THREADS = (CFW_WARPS + 2) * 32, CFW_GRID = 148;
 
 struct CfwParams {
-  static constexpr int KB = CFW_KB, START = 1, SNAP = 2, THREADS = CFW_THREADS;
-  __device__ __forceinline__ int items(const CausalReq& q) const { return static_cast<int>((static_cast<long long>(q.n) * G + CFW_ROWS - 1) / CFW_ROWS); }
-  __device__ __forceinline__ int end(int idx) const { return static_cast<int>((static_cast<long long>(idx) * CFW_ROWS + CFW_ROWS - 1) / G) + 1; }
+  // (WHOLE: the join costs as much as four blocks; one token of 777 keys, 12 heads of 64 over 4: 11.5 us cut, XX us whole)
+  static constexpr int KB = CFW_KB, START = 1, SNAP = 2, WHOLE = 8, THREADS = CFW_THREADS, GRID = CFW_GRID;
+  // rows are counted in 32 bits: the host takes this form below 2^31 rows
+  __device__ __forceinline__ int items(const CausalReq& q) const { return (q.n * G + CFW_ROWS - 1) / CFW_ROWS; }
+  __device__ __forceinline__ int end(int idx) const { return static_cast<int>(static_cast<unsigned>(idx * CFW_ROWS + CFW_ROWS - 1) / static_cast<unsigned>(G)) + 1; }
   __device__ __forceinline__ bool takes(int n) const { return n <= most; }
   CausalParams c;
   float scale_log2e;
@@ -90,7 +92,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
   volatile int* dead = reinterpret_cast<volatile int*>(bars + 3 * ST);
   CausalSpot* spot = reinterpret_cast<CausalSpot*>(bars + 3 * ST + 1);  // [2]
   static_assert((3 * ST + 1) * 8 + 2 * sizeof(CausalSpot) <= 256 + 64, "");
-  long long* weight = reinterpret_cast<long long*>(sK);                 // [CFW_THREADS], ahead of the first load
+  long long* weight = reinterpret_cast<long long*>(sK);                 // a value per warp, ahead of the first load
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -100,6 +102,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
     ptx::prefetch_tmap(&tmK);
     ptx::prefetch_tmap(&tmV);
   }
+  ptx::pdl_wait();
   causal_divide(p, weight, spot);
   ptx::fence_proxy_async();           // the division's scratch becomes the load ring
   __syncthreads();
@@ -344,29 +347,38 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
 template <class T, int DP>
 __global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_constant__ CfwParams p) {
   const int c = blockIdx.x, r = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ptx::pdl_launch();
   ptx::pdl_wait();
   const int4 d = p.desc[2 * c + 1];
   if (d.x == 0) return;
   const CausalReq q = causal_request(p, d.y);
   const int rr = d.w * CFW_ROWS + r, t = rr / p.G;
   if (t >= q.n) return;
-  int last = c;                       // the CTA that ends the item
-  while (last + 1 < CFW_GRID) { ++last; if (p.desc[2 * last].x == 2) break; }
+  const int last = causal_last_part(p.desc, c, CFW_GRID);
   auto slot_of = [&](int i) { return 2LL * i + (i == c ? 1 : 0); };
-  float m = -INFINITY;
-  for (int i = c; i <= last; ++i) if (i == c || p.desc[2 * i].x) m = fmaxf(m, p.part_ml[slot_of(i) * CFW_ROWS + r].x);
   constexpr int PER = DP / 32;
-  float l = 0.f, acc[PER] = {};
-  for (int i = c; i <= last; ++i) {
-    if (i != c && !p.desc[2 * i].x) continue;
-    const float2 ml = p.part_ml[slot_of(i) * CFW_ROWS + r];
-    if (ml.x == -INFINITY) continue;  // a part in which the row saw nothing
-    const float w = exp2f(ml.x - m);
-    l = fmaf(w, ml.y, l);
-    const float* po = p.part_o + (slot_of(i) * CFW_ROWS + r) * DP + lane * PER;
+  float m = -INFINITY, l = 0.f, acc[PER] = {};
+  // a part per lane, 32 at a time; empty slots and parts in which the row saw nothing have the reference -inf
+  auto part = [&](int i) { return i <= last && p.desc[slot_of(i)].x ? p.part_ml[slot_of(i) * CFW_ROWS + r] : make_float2(-INFINITY, 0.f); };
+  for (int i0 = c; i0 <= last; i0 += 32) m = fmaxf(m, part(i0 + lane).x);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = fmaf(w, po[e], acc[e]);
+  for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+  for (int i0 = c; i0 <= last; i0 += 32) {
+    const float2 ml = part(i0 + lane);
+    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+    l += ml.x == -INFINITY ? 0.f : w * ml.y;
+    unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);
+    while (there) {
+      const int e0 = __ffs(there) - 1;
+      there &= there - 1;
+      const float f = __shfl_sync(0xffffffffu, w, e0);
+      const float* po = p.part_o + (slot_of(i0 + e0) * CFW_ROWS + r) * DP + lane * PER;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) acc[e] = fmaf(f, po[e], acc[e]);
+    }
   }
+#pragma unroll
+  for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
   const int seen = q.past + t + 1, head = d.z * p.G + rr - t * p.G;
   const float inv = seen > 0 ? 1.f / l : 0.f;
   bool odd = false;

@@ -50,7 +50,7 @@ constexpr int CTC_START = 3;               // weight of an item's start and end,
 constexpr int CTC_SNAP = 2;                // blocks: cuts closer than this to an item's ends move there
 
 struct CtcParams {
-  static constexpr int KB = CTC_KB, START = CTC_START, SNAP = CTC_SNAP, THREADS = CTC_THREADS;
+  static constexpr int KB = CTC_KB, START = CTC_START, SNAP = CTC_SNAP, WHOLE = 2 * CTC_SNAP, THREADS = CTC_THREADS, GRID = CTC_GRID;
   __device__ __forceinline__ int items(const CausalReq& q) const { return (q.n + 2 * tok - 1) / (2 * tok); }
   __device__ __forceinline__ int end(int idx) const { return (idx + 1) * 2 * tok; }
   __device__ __forceinline__ bool takes(int n) const { return n > past_rows; }
@@ -151,7 +151,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
   CausalSpot* spot = reinterpret_cast<CausalSpot*>(v_free + VS + 1);          // [2]
   static_assert((13 + 2 * KS + 2 * VS) * 8 + 2 * sizeof(CausalSpot) <= 512, "");
-  long long* weight = reinterpret_cast<long long*>(sK);                 // [CTC_THREADS], ahead of the first load
+  long long* weight = reinterpret_cast<long long*>(sK);                 // a value per warp, ahead of the first load
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -559,6 +559,7 @@ __global__ void __launch_bounds__(256) causal_join(const __grid_constant__ CtcPa
   __shared__ float out_s[32][DP + 1];
   __shared__ int odd_s[32];
   const int c = blockIdx.x, t = blockIdx.y >> 2, row = (blockIdx.y & 3) * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ptx::pdl_launch();
   ptx::pdl_wait();
   const int4 d = p.desc[2 * c + 1];
   if (d.x == 0) return;
@@ -567,23 +568,27 @@ __global__ void __launch_bounds__(256) causal_join(const __grid_constant__ CtcPa
   const bool valid = rt < p.tok && t0 + rt < q.n;
   if (threadIdx.x < 32) odd_s[lane] = 0;
   if (!__syncthreads_or(valid)) return;
-  int last = c;                       // the CTA that ends the item
-  while (last + 1 < CTC_GRID) { ++last; if (p.desc[2 * last].x == 2) break; }
-  auto tile_of = [&](int i) { return (2LL * i + (i == c ? 1 : 0)) * 2 + t; };
-  float m = -INFINITY;
-  for (int i = c; i <= last; ++i) if (i == c || p.desc[2 * i].x) m = fmaxf(m, valid ? p.part_ml[tile_of(i) * 128 + row].x : -INFINITY);
+  const int last = causal_last_part(p.desc, c, CTC_GRID);
+  auto slot_of = [&](int i) { return 2LL * i + (i == c ? 1 : 0); };
+  auto tile_of = [&](int i) { return slot_of(i) * 2 + t; };
   constexpr int PER = DP / 8;         // columns of a warp
-  float l = 0.f, acc[PER] = {};
-  for (int i = c; i <= last && valid; ++i) {
-    if (i != c && !p.desc[2 * i].x) continue;
-    const float2 ml = p.part_ml[tile_of(i) * 128 + row];
-    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
-    l = fmaf(w, ml.y, l);
-    const float* po = p.part_o + (tile_of(i) * DP + warp * PER) * 128 + row;
-    if (ml.x != -INFINITY)            // (a part in which the row saw nothing; NaN goes on)
+  float m = -INFINITY, l = 0.f, acc[PER] = {};
+  // parts 32 at a time, the maximum over all of them first
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass)
+#pragma unroll 1
+    for (int i0 = c; i0 <= last; i0 += 32)
+      for (unsigned there = __ballot_sync(0xffffffffu, i0 + lane <= last && p.desc[slot_of(i0 + lane)].x != 0); there; there &= there - 1) {
+        const int i = i0 + __ffs(there) - 1;
+        const float2 ml = valid ? p.part_ml[tile_of(i) * 128 + row] : make_float2(-INFINITY, 0.f);
+        if (pass == 0) { m = fmaxf(m, ml.x); continue; }
+        if (ml.x == -INFINITY) continue;  // a part in which the row saw nothing
+        const float w = exp2f(ml.x - m);
+        l = fmaf(w, ml.y, l);
+        const float* po = p.part_o + (tile_of(i) * DP + warp * PER) * 128 + row;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) if (warp * PER + e < p.n_pv) acc[e] = fmaf(w, po[e * 128], acc[e]);
-  }
+        for (int e = 0; e < PER; ++e) if (warp * PER + e < p.n_pv) acc[e] = fmaf(w, po[e * 128], acc[e]);
+      }
   const int lim = valid ? q.past + t0 + rt + 1 : 0;
   const float inv = lim > 0 ? 1.f / l : 0.f;
   bool odd = false;

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "ptx.cuh"
+
 namespace sod2 {
 namespace k {
 
@@ -37,6 +39,8 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long t0 = static_cast<long long>(blockIdx.x) * PT_TILE;
   const long long t1 = t0 + PT_TILE < p.cap ? t0 + PT_TILE : p.cap;
+  ptx::pdl_launch();
+  ptx::pdl_wait();
   const long long head = p.free_head ? *p.free_head : 0;
   const long long page = p.page;
   long long tok = 0, need = 0;      // totals ahead of this chunk
@@ -157,6 +161,8 @@ template <> __device__ __forceinline__ __nv_bfloat16 rope_store<__nv_bfloat16>(f
 template <class T, int V>
 __global__ void __launch_bounds__(256) rope_store_rows(const __grid_constant__ RopeParams p) {
   extern __shared__ float2 turn_s[];       // [tile][pairs]
+  ptx::pdl_launch();
+  ptx::pdl_wait();
   const int t0 = blockIdx.x * p.tile;
   const int nt = p.n_tokens - t0 < p.tile ? p.n_tokens - t0 : p.tile;
   for (int i = threadIdx.x; i < nt * p.pairs; i += 256) {

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "../../include/sod2.h"
 #include "attention_causal.cuh"
@@ -31,9 +32,9 @@ struct Check {
     return status == SOD2_OK;
   }
   sod2_status fail() { set_thread_error(msg); return status; }
-  sod2_status launched() {
-    const cudaError_t e = cudaGetLastError();
+  sod2_status launched(cudaError_t e) {
     if (e == cudaSuccess) return SOD2_OK;
+    cudaGetLastError();
     status = SOD2_E_CUDA;
     msg = std::string(call) + ": launch failed: " + cudaGetErrorString(e);
     return fail();
@@ -75,8 +76,25 @@ bool vec16(const sod2_pages* r, int esz) {
   return !r || (on(r->data, 16) && r->page_stride * esz % 16 == 0 && r->token_stride * esz % 16 == 0 && r->head_stride * esz % 16 == 0);
 }
 
+// Programmatic dependent launch (ptx.cuh): the kernels of these calls wait for what is before them on the stream ahead of their first access to
+// global memory, and let what is behind them be scheduled while they run.
+template <class... A>
+cudaError_t launch(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const std::decay_t<A>&... a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a...);
+}
+
 template <class T, int V>
-void launch_rope(const k::RopeParams& p, cudaStream_t st) {
+cudaError_t launch_rope(const k::RopeParams& p, cudaStream_t st) {
   const int unit_rows = p.H + p.HK, units = unit_rows * (p.pairs / V + (p.D - 2 * p.pairs) / V);
   k::RopeParams q = p;
   // eight units a thread; fewer where that would leave SMs without a CTA, down to a token, whose heads are then shared out
@@ -87,7 +105,7 @@ void launch_rope(const k::RopeParams& p, cudaStream_t st) {
   int gy = gx < 296 ? 296 / gx : 1;
   const int rounds = (units * q.tile + 255) / 256;
   gy = gy > rounds ? rounds : gy;
-  k::rope_store_rows<T, V><<<dim3(gx, gy < 1 ? 1 : gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st>>>(q);
+  return launch(k::rope_store_rows<T, V>, dim3(gx, gy < 1 ? 1 : gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st, q);
 }
 
 struct AttnCall {
@@ -139,42 +157,25 @@ void set_parts(P& a, const Parts& at, void* ws) {
   a.part_o = reinterpret_cast<float*>(w + at.o);
 }
 
-// the join of cut items, which may be scheduled while the attention ends
-template <class P>
-cudaError_t launch_join(void (*join)(P), dim3 grid, int threads, const P& a, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join, a);
-}
-
 template <class T, int DP>
 cudaError_t launch_tiles(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& a, cudaStream_t st) {
   static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
   if (once != cudaSuccess) return once;
-  k::causal_attention_tcgen05<T, DP><<<k::CTC_GRID, k::CTC_THREADS, k::CtcShape<DP>::SMEM, st>>>(q, kk, v, a);
-  const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess || !a.cut ? e : launch_join(k::causal_join<T, DP>, dim3(k::CTC_GRID, 8), 256, a, st);
+  const cudaError_t e = launch(k::causal_attention_tcgen05<T, DP>, dim3(k::CTC_GRID), k::CTC_THREADS, k::CtcShape<DP>::SMEM, st, q, kk, v, a);
+  return e != cudaSuccess || !a.cut ? e : launch(k::causal_join<T, DP>, dim3(k::CTC_GRID, 8), 256, 0, st, a);
 }
 
 template <class T, int DP>
 cudaError_t launch_few(const CUtensorMap& kk, const CUtensorMap& v, const k::CfwParams& a, cudaStream_t st) {
   static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_few<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CfwShape<DP>::SMEM);
   if (once != cudaSuccess) return once;
-  k::causal_attention_few<T, DP><<<k::CFW_GRID, k::CFW_THREADS, k::CfwShape<DP>::SMEM, st>>>(kk, v, a);
-  const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess || !a.cut ? e : launch_join(k::causal_few_join<T, DP>, dim3(k::CFW_GRID), k::CFW_ROWS * 32, a, st);
+  const cudaError_t e = launch(k::causal_attention_few<T, DP>, dim3(k::CFW_GRID), k::CFW_THREADS, k::CfwShape<DP>::SMEM, st, kk, v, a);
+  return e != cudaSuccess || !a.cut ? e : launch(k::causal_few_join<T, DP>, dim3(k::CFW_GRID), k::CFW_ROWS * 32, 0, st, a);
 }
 
 // max_new, max_keys: the host's bounds on the new tokens (0: none) and the keys of a request.  False where the tensor maps cannot
 // express the operands.
-bool tensor_core_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st) {
+bool tensor_core_attention(const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st, cudaError_t& e) {
   const bool f16 = dtype == SOD2_DTYPE_F16, paged = p.ctx != nullptr;
   const int G = p.H / p.HK;
   if (dtype == SOD2_DTYPE_F32 || p.D > 128 || p.D % 8 || G > 128 || !on(p.q, 16) || !on(p.k, 16) || !on(p.v, 16) || !on(p.o, 16)) return false;
@@ -191,7 +192,7 @@ bool tensor_core_attention(Check& c, const k::CausalParams& p, int dtype, int64_
   if (!encode_16bit_4d(&mk, f16, p.k, ke, ks, kb) || !encode_16bit_4d(&mv, f16, p.v, ke, vs, kb)) return false;
   // Over a cache, requests of up to 16 rows (new tokens x heads of a group) take the few-row form.  It takes all requests where the
   // host's bound says that none has more (one that has more is right there too, and reads its keys once per 16 rows).
-  const int few = paged && G <= k::CFW_ROWS ? k::CFW_ROWS / G : 0;
+  const int few = paged && G <= k::CFW_ROWS && static_cast<int64_t>(p.n_tokens) * G < kMaxRows ? k::CFW_ROWS / G : 0;
   const bool all_few = few > 0 && max_new > 0 && max_new <= few;
   k::CtcParams a{};
   if (!all_few) {
@@ -199,13 +200,13 @@ bool tensor_core_attention(Check& c, const k::CausalParams& p, int dtype, int64_
     const uint32_t qb[4] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(128 / G), 1};
     if (!encode_16bit_4d(&mq, f16, p.q, qe, qs, qb)) return false;
   }
-  cudaError_t e = cudaSuccess;
+  e = cudaSuccess;
   if (few > 0) {
     k::CfwParams b{};
     b.c = p;
     b.scale_log2e = p.scale * 1.4426950408889634f;
     b.G = G; b.ksteps = ksteps; b.box_rows = box_rows;
-    b.cut = max_keys > (2 * k::CfwParams::SNAP - 1) * k::CFW_KB;
+    b.cut = max_keys > (k::CfwParams::WHOLE - 1) * k::CFW_KB;
     b.most = all_few ? 0x7fffffff : few;
     set_parts(b, few_parts(dp), ws);
     if (f16) e = dp == 64 ? launch_few<__half, 64>(mk, mv, b, st) : launch_few<__half, 128>(mk, mv, b, st);
@@ -215,13 +216,12 @@ bool tensor_core_attention(Check& c, const k::CausalParams& p, int dtype, int64_
     a.c = p;
     a.scale_log2e = p.scale * 1.4426950408889634f;
     a.G = G; a.tok = 128 / G; a.ksteps = ksteps; a.n_pv = ksteps * 16; a.box_rows = box_rows;
-    a.cut = max_keys > (2 * k::CtcParams::SNAP - 1) * k::CTC_KB;
+    a.cut = max_keys > (k::CtcParams::WHOLE - 1) * k::CTC_KB;
     a.past_rows = few;
     set_parts(a, tile_parts(dp), ws);
     if (f16) e = dp == 64 ? launch_tiles<__half, 64>(mq, mk, mv, a, st) : launch_tiles<__half, 128>(mq, mk, mv, a, st);
     else e = dp == 64 ? launch_tiles<__nv_bfloat16, 64>(mq, mk, mv, a, st) : launch_tiles<__nv_bfloat16, 128>(mq, mk, mv, a, st);
   }
-  if (e != cudaSuccess) { cudaGetLastError(); c.need(false, SOD2_E_CUDA, cudaGetErrorString(e)); }
   return true;
 }
 
@@ -231,12 +231,13 @@ void check_workspace(Check& c, int dim, const void* ws, size_t bytes) {
   c.need(on(ws, 256), SOD2_E_MISALIGNED, "workspace must be 256-byte aligned");
 }
 
-void launch_attention(Check& c, const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st) {
-  if (tensor_core_attention(c, p, dtype, max_new, max_keys, ws, st)) return;
-  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) * p.H + 3) / 4);
-  if (dtype == SOD2_DTYPE_F32) k::causal_attention_rows<float><<<grid, 128, 0, st>>>(p);
-  else if (dtype == SOD2_DTYPE_F16) k::causal_attention_rows<__half><<<grid, 128, 0, st>>>(p);
-  else k::causal_attention_rows<__nv_bfloat16><<<grid, 128, 0, st>>>(p);
+cudaError_t launch_attention(const k::CausalParams& p, int dtype, int64_t max_new, int64_t max_keys, void* ws, cudaStream_t st) {
+  cudaError_t e;
+  if (tensor_core_attention(p, dtype, max_new, max_keys, ws, st, e)) return e;
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) * p.H + 3) / 4));
+  if (dtype == SOD2_DTYPE_F32) return launch(k::causal_attention_rows<float>, grid, 128, 0, st, p);
+  if (dtype == SOD2_DTYPE_F16) return launch(k::causal_attention_rows<__half>, grid, 128, 0, st, p);
+  return launch(k::causal_attention_rows<__nv_bfloat16>, grid, 128, 0, st, p);
 }
 
 // No exception leaves a C entry: messages are strings, which may fail to allocate.
@@ -276,8 +277,7 @@ extern "C" sod2_status sod2_page_tables(int n_requests, int64_t max_tokens, int 
     int grid = static_cast<int>((max_tokens + k::PT_TILE - 1) / k::PT_TILE);
     const int by_req = (n_requests + 7) / 8 < 148 ? (n_requests + 7) / 8 : 148;
     grid = grid < by_req ? by_req : grid;
-    k::page_tables<<<grid < 1 ? 1 : grid, k::PT_THREADS, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
-    return c.launched();
+    return c.launched(launch(k::page_tables, dim3(grid < 1 ? 1 : grid), k::PT_THREADS, 0, static_cast<cudaStream_t>(cuda_stream), p));
   });
 }
 
@@ -336,10 +336,11 @@ extern "C" sod2_status sod2_rope_store(int dtype, int64_t n_tokens, int n_heads,
     const bool vec = head_dim % V == 0 && n_pairs % V == 0 && vec16(q, esz) && vec16(q_out, esz) && vec16(k, esz) && vec16(k_out, esz) &&
                      vec16(v, esz) && vec16(k_cache, esz) && vec16(v_cache, esz);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dtype == SOD2_DTYPE_F32) { if (vec) launch_rope<float, 4>(p, st); else launch_rope<float, 1>(p, st); }
-    else if (dtype == SOD2_DTYPE_F16) { if (vec) launch_rope<__half, 8>(p, st); else launch_rope<__half, 1>(p, st); }
-    else { if (vec) launch_rope<__nv_bfloat16, 8>(p, st); else launch_rope<__nv_bfloat16, 1>(p, st); }
-    return c.launched();
+    cudaError_t e;
+    if (dtype == SOD2_DTYPE_F32) e = vec ? launch_rope<float, 4>(p, st) : launch_rope<float, 1>(p, st);
+    else if (dtype == SOD2_DTYPE_F16) e = vec ? launch_rope<__half, 8>(p, st) : launch_rope<__half, 1>(p, st);
+    else e = vec ? launch_rope<__nv_bfloat16, 8>(p, st) : launch_rope<__nv_bfloat16, 1>(p, st);
+    return c.launched(e);
   });
 }
 
@@ -375,8 +376,7 @@ extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t 
     p.k = k->data; p.k_ts = k->token_stride; p.k_hs = k->head_stride;
     p.v = v->data; p.v_ts = v->token_stride; p.v_hs = v->head_stride;
     p.status = dev_status;
-    launch_attention(c, p, dtype, 0, n_tokens, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
-    return c.status != SOD2_OK ? c.fail() : c.launched();
+    return c.launched(launch_attention(p, dtype, 0, n_tokens, dev_workspace, static_cast<cudaStream_t>(cuda_stream)));
   });
 }
 
@@ -407,7 +407,6 @@ extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n
     p.v = v_cache->data; p.v_ps = v_cache->page_stride; p.v_ts = v_cache->token_stride; p.v_hs = v_cache->head_stride;
     p.ctx = dev_ctx; p.table = dev_table; p.table_stride = table_stride; p.width = static_cast<int>(table_width);
     p.page = page_size; p.n_pages = static_cast<int>(n_pages); p.status = dev_status;
-    launch_attention(c, p, dtype, max_new, table_width * page_size, dev_workspace, static_cast<cudaStream_t>(cuda_stream));
-    return c.status != SOD2_OK ? c.fail() : c.launched();
+    return c.launched(launch_attention(p, dtype, max_new, table_width * page_size, dev_workspace, static_cast<cudaStream_t>(cuda_stream)));
   });
 }
