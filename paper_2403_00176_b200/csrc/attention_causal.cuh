@@ -33,12 +33,11 @@ __device__ __forceinline__ int causal_cu(const CausalParams& p, int r) {
   const int x = p.cu[r];
   return x < 0 ? 0 : x > p.n_tokens ? p.n_tokens : x;
 }
-__device__ __forceinline__ int causal_ctx(const CausalParams& p, int r, int n) {
-  if (!p.ctx) return n;
-  const int x = p.ctx[r];
+__device__ __forceinline__ int causal_ctx_of(const CausalParams& p, int x) {
   const long long most = static_cast<long long>(p.width) * p.page;
   return x < 0 ? 0 : x > most ? static_cast<int>(most) : x;
 }
+__device__ __forceinline__ int causal_ctx(const CausalParams& p, int r, int n) { return p.ctx ? causal_ctx_of(p, p.ctx[r]) : n; }
 
 // One row of one head by a warp: a lane per key for the scores, then lanes over the head for the weighted sum.  Scores, maximum, sum
 // and output in 32 bits.  `seen`: keys of the request that the row sees; none, and the row is zero.

@@ -16,8 +16,8 @@ template <class P>
 __device__ __forceinline__ CausalReq causal_request(const P& p, int r) {
   CausalReq q;
   q.first = causal_cu(p.c, r);
-  const int n = causal_cu(p.c, r + 1) - q.first;
-  q.past = causal_ctx(p.c, r, n) - n;      // may be negative: the first rows see nothing
+  const int n = causal_cu(p.c, r + 1) - q.first, ctx = p.c.ctx ? p.c.ctx[r] : 0;      // (all three loads on their way together)
+  q.past = (p.c.ctx ? causal_ctx_of(p.c, ctx) : n) - n;      // may be negative: the first rows see nothing
   q.n = n > 0 && p.takes(n) ? n : 0;
   return q;
 }
@@ -159,13 +159,26 @@ __device__ __forceinline__ void causal_divide(const P& p, long long* sums, Causa
       if (pass == 1) {
         if (r0 == 0) {
           if (!many) total = base;
-          at[0] = static_cast<long long>(static_cast<unsigned long long>(total) * blockIdx.x / P::GRID);
-          at[1] = static_cast<long long>(static_cast<unsigned long long>(total) * (blockIdx.x + 1) / P::GRID);
+          if (total < 1 << 23) {
+            at[0] = static_cast<unsigned>(total) * blockIdx.x / P::GRID;
+            at[1] = static_cast<unsigned>(total) * (blockIdx.x + 1) / P::GRID;
+          } else {
+            at[0] = static_cast<long long>(static_cast<unsigned long long>(total) * blockIdx.x / P::GRID);
+            at[1] = static_cast<long long>(static_cast<unsigned long long>(total) * (blockIdx.x + 1) / P::GRID);
+          }
         }
 #pragma unroll 1
         for (int e = 0; e < 2; ++e) {
           const long long x = at[e];
-          const unsigned own = __ballot_sync(0xffffffffu, x >= start && x < start + w);
+          const bool here = x >= start && x < start + w;
+          if (here && np == 1 && w < 1 << 30) {             // an item per head, as single tokens have: no search
+            const unsigned in = static_cast<unsigned>(x - start), one = static_cast<unsigned>(per), head = in / one;
+            const int off = causal_snap<P>(static_cast<int>(in - head * one), static_cast<int>(one) - P::START, p.cut);
+            const long long item = start + head * one;
+            const bool over = off == static_cast<int>(one);
+            spot[e] = CausalSpot{item + off, over ? item + off : item, r, static_cast<int>(head), over ? 1 : 0, over ? 0 : off};
+          }
+          const unsigned own = __ballot_sync(0xffffffffu, here && !(np == 1 && w < 1 << 30));
           if (own) {
             const int src = __ffs(own) - 1;
             const CausalReq o{0, __shfl_sync(0xffffffffu, q.n, src), __shfl_sync(0xffffffffu, q.past, src)};
