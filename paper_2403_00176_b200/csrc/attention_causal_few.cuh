@@ -367,14 +367,24 @@ __global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_co
     const float2 ml = part(i0 + lane);
     const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
     l += ml.x == -INFINITY ? 0.f : w * ml.y;
-    unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);
-    while (there) {
-      const int e0 = __ffs(there) - 1;
-      there &= there - 1;
-      const float f = __shfl_sync(0xffffffffu, w, e0);
-      const float* po = p.part_o + (slot_of(i0 + e0) * CFW_ROWS + r) * DP + lane * PER;
+    const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);
+    // eight parts' rows on their way at a time
+#pragma unroll 1
+    for (int b = 0; b < 32 && i0 + b <= last; b += 8) {
+      float v[8][PER];
 #pragma unroll
-      for (int e = 0; e < PER; ++e) acc[e] = fmaf(f, po[e], acc[e]);
+      for (int k = 0; k < 8; ++k) {
+        const float* po = p.part_o + (slot_of(i0 + b + k) * CFW_ROWS + r) * DP + lane * PER;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[k][e] = there >> (b + k) & 1 ? po[e] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float f = __shfl_sync(0xffffffffu, w, b + k);
+        if (there >> (b + k) & 1)
+#pragma unroll
+          for (int e = 0; e < PER; ++e) acc[e] = fmaf(f, v[k][e], acc[e]);
+      }
     }
   }
 #pragma unroll

@@ -47,10 +47,14 @@ constexpr int CTC_KB = 128;                // keys per block
 constexpr int CTC_CHUNK = 128 * 128;       // bytes of 128 rows x 64 elements
 constexpr int CTC_START = 3;               // weight of an item's start and end, in blocks (1: 908, 2: 1015, 3: 1034 TFLOP/s at 8192 tokens; the first
                                            // items of a head are the shortest, and their CTAs end last where it is too low)
+#ifndef CTC_WHOLE_VALUE
+#define CTC_WHOLE_VALUE 8
+#endif
+constexpr int CTC_WHOLE = CTC_WHOLE_VALUE;               // blocks: shorter items are not cut
 constexpr int CTC_SNAP = 2;                // blocks: cuts closer than this to an item's ends move there
 
 struct CtcParams {
-  static constexpr int KB = CTC_KB, START = CTC_START, SNAP = CTC_SNAP, WHOLE = 2 * CTC_SNAP, THREADS = CTC_THREADS, GRID = CTC_GRID;
+  static constexpr int KB = CTC_KB, START = CTC_START, SNAP = CTC_SNAP, WHOLE = CTC_WHOLE, THREADS = CTC_THREADS, GRID = CTC_GRID;
   __device__ __forceinline__ int items(const CausalReq& q) const { return (q.n + 2 * tok - 1) / (2 * tok); }
   __device__ __forceinline__ int end(int idx) const { return (idx + 1) * 2 * tok; }
   __device__ __forceinline__ bool takes(int n) const { return n > past_rows; }
@@ -552,62 +556,63 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   if (threadIdx.x == 0 && *dead && p.c.status) atomicOr(p.c.status, 1);
 }
 
-// Puts the parts of a cut item together: CTA (c, t, quarter) the 32 rows of tile t of the item that CTA c of the attention began and
-// left unfinished, if any.  out = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i over the parts in their order: the same result every time.
+// Puts the parts of a cut item together: CTA (c, t) tile t of the item that CTA c of the attention began and left unfinished, if any; a
+// thread per row and 16 columns.  out = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i over the parts in their order: the same result every time.
 template <class T, int DP>
-__global__ void __launch_bounds__(256) causal_join(const __grid_constant__ CtcParams p) {
-  __shared__ float out_s[32][DP + 1];
-  __shared__ int odd_s[32];
-  const int c = blockIdx.x, t = blockIdx.y >> 2, row = (blockIdx.y & 3) * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(DP * 8) causal_join(const __grid_constant__ CtcParams p) {
+  __shared__ int odd_s[128];
+  const int c = blockIdx.x, t = blockIdx.y, row = threadIdx.x & 127, d0 = (threadIdx.x >> 7) * 16, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::pdl_launch();
   ptx::pdl_wait();
   const int4 d = p.desc[2 * c + 1];
   if (d.x == 0) return;
   const CausalReq q = causal_request(p, d.y);
   const int t0 = (2 * d.w + t) * p.tok, rt = row / p.G;
+  if (t0 >= q.n) return;
   const bool valid = rt < p.tok && t0 + rt < q.n;
-  if (threadIdx.x < 32) odd_s[lane] = 0;
-  if (!__syncthreads_or(valid)) return;
+  if (threadIdx.x < 128) odd_s[threadIdx.x] = 0;
+  __syncthreads();
   const int last = causal_last_part(p.desc, c, CTC_GRID);
   auto slot_of = [&](int i) { return 2LL * i + (i == c ? 1 : 0); };
-  auto tile_of = [&](int i) { return slot_of(i) * 2 + t; };
-  constexpr int PER = DP / 8;         // columns of a warp
-  float m = -INFINITY, l = 0.f, acc[PER] = {};
+  float m = -INFINITY, l = 0.f, acc[16] = {};
   // parts 32 at a time, the maximum over all of them first
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass)
 #pragma unroll 1
     for (int i0 = c; i0 <= last; i0 += 32)
       for (unsigned there = __ballot_sync(0xffffffffu, i0 + lane <= last && p.desc[slot_of(i0 + lane)].x != 0); there; there &= there - 1) {
-        const int i = i0 + __ffs(there) - 1;
-        const float2 ml = valid ? p.part_ml[tile_of(i) * 128 + row] : make_float2(-INFINITY, 0.f);
+        const long long tile = slot_of(i0 + __ffs(there) - 1) * 2 + t;
+        const float2 ml = valid ? p.part_ml[tile * 128 + row] : make_float2(-INFINITY, 0.f);
         if (pass == 0) { m = fmaxf(m, ml.x); continue; }
         if (ml.x == -INFINITY) continue;  // a part in which the row saw nothing
         const float w = exp2f(ml.x - m);
         l = fmaf(w, ml.y, l);
-        const float* po = p.part_o + (tile_of(i) * DP + warp * PER) * 128 + row;
+        const float* po = p.part_o + (tile * DP + d0) * 128 + row;
+        if (d0 < p.n_pv)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) if (warp * PER + e < p.n_pv) acc[e] = fmaf(w, po[e * 128], acc[e]);
+          for (int e = 0; e < 16; ++e) acc[e] = fmaf(w, po[e * 128], acc[e]);
       }
-  const int lim = valid ? q.past + t0 + rt + 1 : 0;
+  const int lim = q.past + t0 + rt + 1;
   const float inv = lim > 0 ? 1.f / l : 0.f;
   bool odd = false;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) {
-    const float x = acc[e] * inv;
-    odd |= warp * PER + e < p.c.D && !(fabsf(x) < INFINITY);
-    out_s[lane][warp * PER + e] = x;
+  for (int e = 0; e < 16; ++e) { acc[e] *= inv; odd |= !(fabsf(acc[e]) < INFINITY); }
+  const int h = d.z * p.G + row - rt * p.G, orow = q.first + t0 + rt;
+  if (valid && d0 < p.c.D) {
+    if (odd) {
+      odd_s[row] = 1;
+    } else {
+      uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(p.c.o) + orow * p.c.o_ts + h * p.c.o_hs + d0);
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = CtcType<T>::pack(acc[2 * e], acc[2 * e + 1]);
+      o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (d0 + 8 < p.c.D) o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
   }
-  if (odd && valid) odd_s[lane] = 1;
   __syncthreads();
-  for (int r = warp; r < 32; r += 8) {
-    const int rr = (blockIdx.y & 3) * 32 + r, tt = rr / p.G;
-    if (tt >= p.tok || t0 + tt >= q.n) continue;
-    const int h = d.z * p.G + rr - tt * p.G, orow = q.first + t0 + tt;
-    if (odd_s[r]) { causal_row<T>(p.c, d.y, q.first, orow, h, q.past + t0 + tt + 1, 0, 1); continue; }
-    T* o = static_cast<T*>(p.c.o) + orow * p.c.o_ts + h * p.c.o_hs;
-    for (int e = lane; e < p.c.D; e += 32) o[e] = rope_store<T>(out_s[r][e]);
-  }
+  for (int r = warp; r < 128; r += DP / 4)      // rows whose result is not finite: key by key
+    if (odd_s[r]) causal_row<T>(p.c, d.y, q.first, q.first + t0 + r / p.G, d.z * p.G + r % p.G, q.past + t0 + r / p.G + 1, 0, 1);
 }
 
 }  // namespace k

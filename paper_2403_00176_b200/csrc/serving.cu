@@ -162,7 +162,7 @@ cudaError_t launch_tiles(const CUtensorMap& q, const CUtensorMap& kk, const CUte
   static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
   if (once != cudaSuccess) return once;
   const cudaError_t e = launch(k::causal_attention_tcgen05<T, DP>, dim3(k::CTC_GRID), k::CTC_THREADS, k::CtcShape<DP>::SMEM, st, q, kk, v, a);
-  return e != cudaSuccess || !a.cut ? e : launch(k::causal_join<T, DP>, dim3(k::CTC_GRID, 8), 256, 0, st, a);
+  return e != cudaSuccess || !a.cut ? e : launch(k::causal_join<T, DP>, dim3(k::CTC_GRID, 2), DP * 8, 0, st, a);
 }
 
 template <class T, int DP>
