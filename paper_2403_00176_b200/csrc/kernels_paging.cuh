@@ -31,36 +31,40 @@ constexpr int PT_TILE = 1024;       // rows of the slot map per CTA
 // list at head + sum over s < r of (want_s - have_s).  Two prefix sums over the requests give that and the packed row of each
 // request; every CTA makes both over all requests (8 bytes a request, out of L2) instead of a launch that hands them on,
 // then fills its own tile of rows and every gridDim-th request's table entries.  A new token's page is looked up where the
-// table's new entry comes from, not in the table, which other CTAs are writing.  Sums are 64-bit: lengths are any int.
+// table's new entry comes from, not in the table, which other CTAs are writing.  Sums are 64-bit; a position, at most the sum of two
+// ints, is an unsigned of 32 bits.
 __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant__ PageTableParams p) {
   __shared__ long long cu_s[PT_CHUNK + 1], need_s[PT_CHUNK + 1];
-  __shared__ int past_s[PT_CHUNK];
+  __shared__ unsigned past_s[PT_CHUNK];
   __shared__ long long warp_s[2][PT_THREADS / 32];
+  ptx::pdl_launch();
+  ptx::pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long t0 = static_cast<long long>(blockIdx.x) * PT_TILE;
   const long long t1 = t0 + PT_TILE < p.cap ? t0 + PT_TILE : p.cap;
-  ptx::pdl_launch();
-  ptx::pdl_wait();
   const long long head = p.free_head ? *p.free_head : 0;
-  const long long page = p.page;
+  const unsigned page = p.page;
+  auto pages = [&](unsigned n) { const unsigned q = n / page; return q + (n != q * page); };
   long long tok = 0, need = 0;      // totals ahead of this chunk
   int bad = 0;
+#pragma unroll 1
   for (int c0 = 0; c0 < p.n_req; c0 += PT_CHUNK) {
     long long tv[4], nv[4], ts = 0, ns = 0;
+    int ra[4], rb[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int i = tid * 4 + e, r = c0 + i;
-      long long a = 0, b = 0;
-      if (r < p.n_req) {
-        const int ra = p.past[r], rb = p.fresh[r];
-        if (ra < 0 || rb < 0) bad |= SERVE_BAD_LENGTH;
-        a = ra < 0 ? 0 : ra;
-        b = rb < 0 ? 0 : rb;
-        past_s[i] = static_cast<int>(a);
-      }
+      const int r = c0 + tid * 4 + e;
+      ra[e] = r < p.n_req ? p.past[r] : 0;
+      rb[e] = r < p.n_req ? p.fresh[r] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (ra[e] < 0 || rb[e] < 0) bad |= SERVE_BAD_LENGTH;
+      const unsigned a = ra[e] < 0 ? 0 : ra[e], b = rb[e] < 0 ? 0 : rb[e];
+      past_s[tid * 4 + e] = a;
       tv[e] = ts; nv[e] = ns;
       ts += b;
-      ns += (a + b + page - 1) / page - (a + page - 1) / page;
+      ns += pages(a + b) - pages(a);
     }
     long long ti = ts, ni = ns;     // inclusive over the warp's threads
 #pragma unroll
@@ -71,6 +75,7 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant_
     if (lane == 31) { warp_s[0][warp] = ti; warp_s[1][warp] = ni; }
     __syncthreads();
     long long tb = tok + ti - ts, nb = need + ni - ns;
+#pragma unroll
     for (int w = 0; w < PT_THREADS / 32; ++w) {
       if (w < warp) { tb += warp_s[0][w]; nb += warp_s[1][w]; }
       tok += warp_s[0][w]; need += warp_s[1][w];
@@ -82,8 +87,10 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant_
     const int nr = p.n_req - c0 < PT_CHUNK ? p.n_req - c0 : PT_CHUNK;
     // tables, cumulative lengths and contexts: requests in turn over all warps of the grid
     const int step = gridDim.x * (PT_THREADS / 32);
+#pragma unroll 1
     for (int i = blockIdx.x * (PT_THREADS / 32) + warp; i < nr; i += step) {
-      const long long a = past_s[i], n = cu_s[i + 1] - cu_s[i], have = (a + page - 1) / page, k = need_s[i + 1] - need_s[i];
+      const unsigned a = past_s[i], have = pages(a);
+      const long long n = cu_s[i + 1] - cu_s[i], k = need_s[i + 1] - need_s[i];
       for (long long j = lane; j < k; j += 32) {
         const long long f = head + need_s[i] + j;
         int id = -1;
@@ -99,17 +106,24 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant_
     }
     // slots and positions of this CTA's rows that belong to the chunk's requests
     const long long lo = t0 > cu_s[0] ? t0 : cu_s[0], hi = t1 < cu_s[nr] ? t1 : cu_s[nr];
-    for (long long t = lo + tid; t < hi; t += PT_THREADS) {
-      int a = 0, b = nr;            // last request whose first row is not behind t; empty requests share a first row
-      while (b - a > 1) { const int m = (a + b) >> 1; if (cu_s[m] <= t) a = m; else b = m; }
-      const long long pos = past_s[a] + (t - cu_s[a]), j = pos / page, have = (past_s[a] + page - 1) / page;
-      int id = -1;
-      if (j < p.width) {
-        if (j < have) id = p.table[(c0 + a) * p.table_stride + j];
-        else { const long long f = head + need_s[a] + (j - have); if (f >= 0 && f < p.n_free) id = p.free_pages[f]; }
+    if (lo < hi) {
+      // last request whose first row is not behind t (empty requests share a first row), among those of the tile
+      auto request = [&](long long t, int a, int b) {
+        while (b - a > 1) { const int m = (a + b) >> 1; if (cu_s[m] <= t) a = m; else b = m; }
+        return a;
+      };
+      const int r0 = request(lo, 0, nr), r1 = request(hi - 1, r0, nr) + 1;
+      for (long long t = lo + tid; t < hi; t += PT_THREADS) {
+        const int a = request(t, r0, r1);
+        const unsigned pos = past_s[a] + static_cast<unsigned>(t - cu_s[a]), j = pos / page, have = pages(past_s[a]);
+        int id = -1;
+        if (j < static_cast<unsigned>(p.width)) {
+          if (j < have) id = p.table[(c0 + a) * p.table_stride + j];
+          else { const long long f = head + need_s[a] + (j - have); if (f >= 0 && f < p.n_free) id = p.free_pages[f]; }
+        }
+        if (p.positions) p.positions[t] = static_cast<int>(pos < 0x7fffffffu ? pos : 0x7fffffffu);
+        p.slots[t] = id < 0 ? -1 : static_cast<long long>(id) * page + (pos - j * page);
       }
-      if (p.positions) p.positions[t] = static_cast<int>(pos < 0x7fffffff ? pos : 0x7fffffff);
-      p.slots[t] = id < 0 ? -1 : static_cast<long long>(id) * page + (pos - j * page);
     }
     __syncthreads();
   }
@@ -137,7 +151,7 @@ struct RopeParams {
   long long q_ts, q_hs, qo_ts, qo_hs, k_ts, k_hs, ko_ts, ko_hs, v_ts, v_hs, pos_stride;
   long long kc_ps, kc_ts, kc_hs, vc_ps, vc_ts, vc_hs;
   long long n_slots;
-  int n_tokens, H, HK, D, pairs, adjacent, page, tile;
+  int n_tokens, H, HK, D, pairs, adjacent, page, tile, split;
   double turns[ROPE_MAX_PAIRS];           // turns per position of each pair: frequency / 2 pi
   unsigned char axis[ROPE_MAX_PAIRS];
 };
@@ -152,100 +166,169 @@ template <> __device__ __forceinline__ float rope_store<float>(float x) { return
 template <> __device__ __forceinline__ __half rope_store<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 rope_store<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// Two neighbouring elements as two floats and back: one instruction a float, one for the rounding of both.
+__device__ __forceinline__ float2 rope_pair(const float* v) { return make_float2(v[0], v[1]); }
+__device__ __forceinline__ float2 rope_pair(const __half* v) { return __half22float2(*reinterpret_cast<const __half2*>(v)); }
+__device__ __forceinline__ float2 rope_pair(const __nv_bfloat16* v) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(v);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ void rope_pack(float* v, float2 f) { v[0] = f.x; v[1] = f.y; }
+__device__ __forceinline__ void rope_pack(__half* v, float2 f) { *reinterpret_cast<__half2*>(v) = __floats2half2_rn(f.x, f.y); }
+__device__ __forceinline__ void rope_pack(__nv_bfloat16* v, float2 f) { *reinterpret_cast<__nv_bfloat162*>(v) = __floats2bfloat162_rn(f.x, f.y); }
+
+// The V pairs of one unit, turned: x[e] with y[e] (adjacent == 0), or x first, then y, neighbours with each other.  Two operations an
+// instruction: with one, the instructions bound the kernel (40320 tokens, 24 heads of 64: 63 us against 54).
+template <class T, int V>
+__device__ __forceinline__ void rope_turn(RopeVec<T, V>& x, RopeVec<T, V>& y, const float* c, const float* s, bool adjacent) {
+  if constexpr (V == 1) {
+    const float u = rope_load(x.e[0]), w = rope_load(y.e[0]);
+    x.e[0] = rope_store<T>(u * c[0] - w * s[0]);
+    y.e[0] = rope_store<T>(w * c[0] + u * s[0]);
+  } else if (!adjacent) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+      const float2 u = rope_pair(x.e + e), w = rope_pair(y.e + e), cc = make_float2(c[e], c[e + 1]), ss = make_float2(s[e], s[e + 1]);
+      const float2 ws = ptx::mul_x2(w, ss);
+      rope_pack(x.e + e, ptx::fma_x2(u, cc, make_float2(-ws.x, -ws.y)));
+      rope_pack(y.e + e, ptx::fma_x2(w, cc, ptx::mul_x2(u, ss)));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      T* v = e < V / 2 ? x.e + 2 * e : y.e + 2 * e - V;
+      const float2 u = rope_pair(v);
+      rope_pack(v, ptx::fma_x2(u, make_float2(c[e], c[e]), ptx::mul_x2(make_float2(u.y, u.x), make_float2(-s[e], s[e]))));
+    }
+  }
+}
+
 // (x, y) -> (x cos a - y sin a, y cos a + x sin a) with a = position * frequency, for every pair of every query and key head of
 // a token; values go to the cache as they are.  One pass over the rows: nothing but them moves, so memory bounds it.
 // The angle is reduced in 64 bits: at position 10^6 a 32-bit product is off by 0.06 radians.  What is left of it, at most
 // half a turn, goes into sincospif in 32 bits (2^-24 relative).  Rotated values are rounded once, to the type of the rows.
-// A CTA takes `tile` tokens (and one of gridDim.y shares of their heads): the angles of its tokens go to shared memory once, for all heads.
-// A thread keeps one place in the head (V elements and the V they are paired with: 16 bytes each) over the heads it takes.
+// A CTA takes `tile` tokens and one of gridDim.y shares of their heads, queries and keys in one list.  A thread keeps a token and a place in the
+// head (V pairs: 16 bytes of each side) and goes through heads `split` apart, two at a time.  Everything that does not hang on the angles is on its way
+// before they are worked out: a CTA's life is then one trip to memory and back and not four.
 template <class T, int V>
-__global__ void __launch_bounds__(256) rope_store_rows(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(256, 4) rope_store_rows(const __grid_constant__ RopeParams p) {
   extern __shared__ float2 turn_s[];       // [tile][pairs]
+  using Vec = RopeVec<T, V>;
+  constexpr int B = 2;
   ptx::pdl_launch();
   ptx::pdl_wait();
   const int t0 = blockIdx.x * p.tile;
   const int nt = p.n_tokens - t0 < p.tile ? p.n_tokens - t0 : p.tile;
-  for (int i = threadIdx.x; i < nt * p.pairs; i += 256) {
-    const int t = i / p.pairs, j = i - t * p.pairs;
-    const double x = p.turns[j] * static_cast<double>(p.positions[p.axis[j] * p.pos_stride + t0 + t]);
-    float s, c;
-    sincospif(2.f * static_cast<float>(x - rint(x)), &s, &c);
-    turn_s[i] = make_float2(c, s);
+  const int U = p.pairs / V, unit = threadIdx.x % U, place = threadIdx.x / U, t = place / p.split, share = place - t * p.split;
+  const int HT = p.H + p.HK, step = p.split * gridDim.y;
+  const int h0 = t < nt ? blockIdx.y * p.split + share : HT;     // the thread's first head
+  const int a = p.adjacent ? unit * 2 * V : unit * V, b = p.adjacent ? a + V : a + p.pairs;
+  const long long row = t0 + (t < nt ? t : 0);
+  const T* q = static_cast<const T*>(p.q) + row * p.q_ts;
+  const T* k = static_cast<const T*>(p.k) + row * p.k_ts - p.H * p.k_hs;     // (indexed from head H on)
+  Vec x[B], y[B];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int e = 0; e < B; ++e) {
+      const int hh = h + e * step;
+      if (hh < HT) {
+        const T* src = hh < p.H ? q + hh * p.q_hs : k + hh * p.k_hs;
+        x[e] = *reinterpret_cast<const Vec*>(src + a);
+        y[e] = *reinterpret_cast<const Vec*>(src + b);
+      }
+    }
+  };
+  // the position of the thread's first angle, its token's slot, its rows, its first values
+  const int n_angles = nt * p.pairs, a0 = threadIdx.x / p.pairs, j0 = threadIdx.x - a0 * p.pairs;
+  const int pos0 = threadIdx.x < n_angles ? p.positions[p.axis[j0] * p.pos_stride + t0 + a0] : 0;
+  const long long slot = p.slots && t < nt ? p.slots[row] : -1;
+  load(h0);
+  auto place_of = [&](long long sl, long long ps, long long ts) {
+    if (sl < 0 || sl >= p.n_slots) return -1ll;
+    const long long page = sl / p.page;
+    return page * ps + (sl - page * p.page) * ts;
+  };
+  const int vu = p.D / V, n_values = p.vc ? nt * p.HK * vu : 0, v_step = 256 * gridDim.y;
+  Vec val[2];
+  long long to[2];
+  auto load_values = [&](int i0) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = i0 + e * v_step;
+      to[e] = -1;
+      if (i < n_values) {
+        const int r = i / vu, u = i - r * vu, tt = r / p.HK, h = r - tt * p.HK;
+        const long long at = place_of(p.slots[t0 + tt], p.vc_ps, p.vc_ts);
+        val[e] = *reinterpret_cast<const Vec*>(static_cast<const T*>(p.v) + (t0 + tt) * p.v_ts + h * p.v_hs + u * V);
+        to[e] = at < 0 ? -1 : at + h * p.vc_hs + u * V;
+      }
+    }
+  };
+  const int v0 = blockIdx.y * 256 + threadIdx.x;
+  load_values(v0);
+  for (int i = threadIdx.x; i < n_angles; i += 256) {
+    const int tt = i / p.pairs, j = i - tt * p.pairs;
+    const int pos = i == static_cast<int>(threadIdx.x) ? pos0 : p.positions[p.axis[j] * p.pos_stride + t0 + tt];
+    const double angle = p.turns[j] * static_cast<double>(pos);
+    float sn, cn;
+    sincospif(2.f * static_cast<float>(angle - rint(angle)), &sn, &cn);
+    turn_s[i] = make_float2(cn, sn);
   }
+  for (int i = v0; i < n_values;) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) if (to[e] >= 0) *reinterpret_cast<Vec*>(static_cast<T*>(p.vc) + to[e]) = val[e];
+    i += 2 * v_step;
+    load_values(i);
+  }
+  const long long kc = p.kc ? place_of(slot, p.kc_ps, p.kc_ts) : -1;
   __syncthreads();
-  using Vec = RopeVec<T, V>;
-  // units of a query or key head: `ru` of two vectors that are rotated, then single vectors that are copied
-  const int ru = p.pairs / V, rot = 2 * p.pairs, cu = (p.D - rot) / V, U = ru + cu;
-  const int HT = p.H + p.HK, rows = nt * HT;
-  if (U > 0) {
-    const int unit = threadIdx.x % U, per = 256 / U, slot = threadIdx.x / U;
-    if (slot < per) {
-      for (int i = blockIdx.y * per + slot; i < rows; i += per * gridDim.y) {
-        const int t = i / HT, h = i - t * HT;
-        const long long row = t0 + t;
-        const T* src; T* dst; T* dst2 = nullptr;
-        if (h < p.H) {
-          src = static_cast<const T*>(p.q) + row * p.q_ts + h * p.q_hs;
-          dst = static_cast<T*>(p.q_out) + row * p.qo_ts + h * p.qo_hs;
-        } else {
-          src = static_cast<const T*>(p.k) + row * p.k_ts + (h - p.H) * p.k_hs;
-          dst = p.k_out ? static_cast<T*>(p.k_out) + row * p.ko_ts + (h - p.H) * p.ko_hs : nullptr;
-          if (p.kc) {
-            const long long s = p.slots[row];
-            if (s >= 0 && s < p.n_slots) dst2 = static_cast<T*>(p.kc) + (s / p.page) * p.kc_ps + (s % p.page) * p.kc_ts + (h - p.H) * p.kc_hs;
-          }
-        }
-        if (unit < ru) {
-          const int a = p.adjacent ? unit * 2 * V : unit * V, b = p.adjacent ? a + V : a + p.pairs;
-          Vec x = *reinterpret_cast<const Vec*>(src + a), y = *reinterpret_cast<const Vec*>(src + b);
-          const float2* cs = turn_s + t * p.pairs + unit * V;
-          if (p.adjacent) {
-            if constexpr (V == 1) {
-              const float u = rope_load(x.e[0]), w = rope_load(y.e[0]);
-              x.e[0] = rope_store<T>(u * cs[0].x - w * cs[0].y);
-              y.e[0] = rope_store<T>(w * cs[0].x + u * cs[0].y);
-            } else {
+  if (share == 0 && unit == 0 && blockIdx.y == 0 && slot >= p.n_slots && p.status) atomicOr(p.status, SERVE_BAD_PAGE);
+  float c[V], s[V];
 #pragma unroll
-              for (int e = 0; e < V / 2; ++e) {
-                float u = rope_load(x.e[2 * e]), w = rope_load(x.e[2 * e + 1]);
-                float2 c = cs[e];
-                x.e[2 * e] = rope_store<T>(u * c.x - w * c.y);
-                x.e[2 * e + 1] = rope_store<T>(w * c.x + u * c.y);
-                u = rope_load(y.e[2 * e]); w = rope_load(y.e[2 * e + 1]);
-                c = cs[V / 2 + e];
-                y.e[2 * e] = rope_store<T>(u * c.x - w * c.y);
-                y.e[2 * e + 1] = rope_store<T>(w * c.x + u * c.y);
-              }
-            }
-          } else {
+  for (int e = 0; e < V; ++e) { const float2 cs = turn_s[(t < nt ? t : 0) * p.pairs + unit * V + e]; c[e] = cs.x; s[e] = cs.y; }
+  T* qo = static_cast<T*>(p.q_out) + row * p.qo_ts;
+  T* ko = static_cast<T*>(p.k_out) + row * p.ko_ts - p.H * p.ko_hs;
+  T* kd = static_cast<T*>(p.kc) + kc - p.H * p.kc_hs;
+#pragma unroll 1
+  for (int h = h0; h < HT;) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float u = rope_load(x.e[e]), w = rope_load(y.e[e]);
-              x.e[e] = rope_store<T>(u * cs[e].x - w * cs[e].y);
-              y.e[e] = rope_store<T>(w * cs[e].x + u * cs[e].y);
-            }
-          }
-          if (dst) { *reinterpret_cast<Vec*>(dst + a) = x; *reinterpret_cast<Vec*>(dst + b) = y; }
-          if (dst2) { *reinterpret_cast<Vec*>(dst2 + a) = x; *reinterpret_cast<Vec*>(dst2 + b) = y; }
+    for (int e = 0; e < B; ++e) {
+      const int hh = h + e * step;
+      if (hh < HT) {
+        rope_turn<T, V>(x[e], y[e], c, s, p.adjacent);
+        if (hh < p.H) {
+          *reinterpret_cast<Vec*>(qo + hh * p.qo_hs + a) = x[e];
+          *reinterpret_cast<Vec*>(qo + hh * p.qo_hs + b) = y[e];
         } else {
-          const int a = rot + (unit - ru) * V;
-          const Vec x = *reinterpret_cast<const Vec*>(src + a);
-          if (dst) *reinterpret_cast<Vec*>(dst + a) = x;
-          if (dst2) *reinterpret_cast<Vec*>(dst2 + a) = x;
+          if (p.k_out) {
+            *reinterpret_cast<Vec*>(ko + hh * p.ko_hs + a) = x[e];
+            *reinterpret_cast<Vec*>(ko + hh * p.ko_hs + b) = y[e];
+          }
+          if (kc >= 0) {
+            *reinterpret_cast<Vec*>(kd + hh * p.kc_hs + a) = x[e];
+            *reinterpret_cast<Vec*>(kd + hh * p.kc_hs + b) = y[e];
+          }
         }
       }
     }
+    h += B * step;
+    load(h);
   }
-  if (!p.vc && !p.kc) return;
-  // values, and what the slots say
-  const int vu = p.D / V;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * p.HK * vu; i += 256 * gridDim.y) {
-    const int r = i / vu, u = i - r * vu, t = r / p.HK, h = r - t * p.HK;
-    const long long row = t0 + t, s = p.slots[row];
-    if (s >= p.n_slots && p.status && u == 0 && h == 0) atomicOr(p.status, SERVE_BAD_PAGE);
-    if (!p.vc || s < 0 || s >= p.n_slots) continue;
-    const Vec x = *reinterpret_cast<const Vec*>(static_cast<const T*>(p.v) + row * p.v_ts + h * p.v_hs + u * V);
-    *reinterpret_cast<Vec*>(static_cast<T*>(p.vc) + (s / p.page) * p.vc_ps + (s % p.page) * p.vc_ts + h * p.vc_hs + u * V) = x;
+  // what lies behind the turned pairs, copied
+  const int rot = 2 * p.pairs, cu = (p.D - rot) / V;
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * HT * cu; i += 256 * gridDim.y) {
+    const int r = i / cu, u = rot + (i - r * cu) * V, tt = r / HT, h = r - tt * HT;
+    const long long rr = t0 + tt;
+    if (h < p.H) {
+      *reinterpret_cast<Vec*>(static_cast<T*>(p.q_out) + rr * p.qo_ts + h * p.qo_hs + u) = *reinterpret_cast<const Vec*>(static_cast<const T*>(p.q) + rr * p.q_ts + h * p.q_hs + u);
+    } else {
+      const Vec v = *reinterpret_cast<const Vec*>(static_cast<const T*>(p.k) + rr * p.k_ts + (h - p.H) * p.k_hs + u);
+      if (p.k_out) *reinterpret_cast<Vec*>(static_cast<T*>(p.k_out) + rr * p.ko_ts + (h - p.H) * p.ko_hs + u) = v;
+      if (p.kc) {
+        const long long at = place_of(p.slots[rr], p.kc_ps, p.kc_ts);
+        if (at >= 0) *reinterpret_cast<Vec*>(static_cast<T*>(p.kc) + at + (h - p.H) * p.kc_hs + u) = v;
+      }
+    }
   }
 }
 

@@ -95,17 +95,19 @@ cudaError_t launch(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cu
 
 template <class T, int V>
 cudaError_t launch_rope(const k::RopeParams& p, cudaStream_t st) {
-  const int unit_rows = p.H + p.HK, units = unit_rows * (p.pairs / V + (p.D - 2 * p.pairs) / V);
+  const int heads = p.H + p.HK, places = 256 / (p.pairs / V);
   k::RopeParams q = p;
-  // eight units a thread; fewer where that would leave SMs without a CTA, down to a token, whose heads are then shared out
-  const int most = (p.n_tokens + 148 * 4 - 1) / (148 * 4), want = units > 0 ? 2048 / units : 1;
-  q.tile = want < most ? want : most;
-  q.tile = q.tile < 1 ? 1 : q.tile > 32 ? 32 : q.tile;
+  // Four heads a thread.  Fewer where that would leave SMs without a CTA: then fewer tokens a CTA, down to one, and heads shared out
+  // further, over CTAs too.
+  q.split = (heads + 3) / 4 < places ? (heads + 3) / 4 : places;
+  const int spread = (p.n_tokens + 2 * 148 - 1) / (2 * 148);
+  q.tile = places / q.split;
+  if (q.tile > spread) { q.tile = spread; q.split = places / q.tile < heads ? places / q.tile : heads; }
   const int gx = (p.n_tokens + q.tile - 1) / q.tile;
-  int gy = gx < 296 ? 296 / gx : 1;
-  const int rounds = (units * q.tile + 255) / 256;
-  gy = gy > rounds ? rounds : gy;
-  return launch(k::rope_store_rows<T, V>, dim3(gx, gy < 1 ? 1 : gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st, q);
+  int gy = gx < 2 * 148 ? 2 * 148 / gx : 1;
+  const int most = (heads + q.split - 1) / q.split;
+  gy = gy > most ? most : gy;
+  return launch(k::rope_store_rows<T, V>, dim3(gx, gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st, q);
 }
 
 struct AttnCall {
