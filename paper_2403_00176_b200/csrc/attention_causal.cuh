@@ -34,7 +34,7 @@ __device__ __forceinline__ int causal_cu(const CausalParams& p, int r) {
   return x < 0 ? 0 : x > p.n_tokens ? p.n_tokens : x;
 }
 __device__ __forceinline__ int causal_ctx_of(const CausalParams& p, int x) {
-  const long long most = static_cast<long long>(p.width) * p.page;
+  const long long all = static_cast<long long>(p.width) * p.page, most = all < 0x7fffff00 ? all : 0x7fffff00;      // (blocks of keys are counted in ints)
   return x < 0 ? 0 : x > most ? static_cast<int>(most) : x;
 }
 __device__ __forceinline__ int causal_ctx(const CausalParams& p, int r, int n) { return p.ctx ? causal_ctx_of(p, p.ctx[r]) : n; }

@@ -5,7 +5,7 @@
 // (one per SM) share the items' blocks evenly, as attention_causal_division.cuh describes, and causal_few_join puts cut items together.
 // With 16 rows a tcgen05.mma would leave seven eighths of its 128 rows empty and the scores in one warp's quarter of TMEM, so the products are
 // mma.sync m16n8k16: 2 x 64 of them a block of 128 keys and head size 128, an eighth of it per warp, beside 64 KB of loads.
-//   warps 0..7  16 of the block's 128 keys each: S = Q K^T (16 x 16), P = 2^(S c - m), O += P V, with a maximum, sum and O of their own in
+//   warps 0..7  16 keys of the block each (twice at head size 64): S = Q K^T (16 x 16), P = 2^(S c - m), O += P V, with a maximum, sum and O of their own in
 //               registers; no exchange until the item ends, where the eight are put together through shared memory
 //   warp 8 / 9  load K / V: a box per page and 64 columns, lanes side by side
 // Maximum, sum and O are 32-bit, P is rounded once to the type of the values.  The exponent reference moves only when a score exceeds it by
@@ -19,11 +19,15 @@
 namespace sod2 {
 namespace k {
 
-constexpr int CFW_ROWS = 16, CFW_KB = 128, CFW_WARPS = 8, CFW_THREADS = (CFW_WARPS + 2) * 32, CFW_GRID = 148;
+constexpr int CFW_ROWS = 16, CFW_WARPS = 8, CFW_THREADS = (CFW_WARPS + 2) * 32, CFW_GRID = 148;
 
+// Blocks of 64 KB: 128 keys of head size up to 128, 256 of up to 64 (with 128 there, half as many lanes issue boxes and the TMA unit is short of
+// them: 64 conversations of 2000 keys, 12 heads of 64 over 4, 34.0 us against 31.5).
+template <int DP>
 struct CfwParams {
-  // (WHOLE: the join costs as much as four blocks; one token of 777 keys, 12 heads of 64 over 4: 11.5 us cut, XX us whole)
-  static constexpr int KB = CFW_KB, START = 1, SNAP = 2, WHOLE = 8, THREADS = CFW_THREADS, GRID = CFW_GRID;
+  // START 1, 2, 3: 64 conversations of 100 to 8000 keys, 32 heads of 128 over 8, 88.4, 78.9, 78.7 us.  WHOLE 8, 4: one token of 777 keys
+  // 12.9, 10.8 us
+  static constexpr int KB = 16384 / DP, START = 2, SNAP = 2, WHOLE = 4, THREADS = CFW_THREADS, GRID = CFW_GRID;
   // rows are counted in 32 bits: the host takes this form below 2^31 rows
   __device__ __forceinline__ int items(const CausalReq& q) const { return (q.n * G + CFW_ROWS - 1) / CFW_ROWS; }
   __device__ __forceinline__ int end(int idx) const { return static_cast<int>(static_cast<unsigned>(idx * CFW_ROWS + CFW_ROWS - 1) / static_cast<unsigned>(G)) + 1; }
@@ -38,8 +42,9 @@ struct CfwParams {
 };
 
 template <int DP> struct CfwShape {
-  static constexpr int NC = DP / 64, CHUNK = CFW_KB * 128, TILE = NC * CHUNK;      // K or V of a block
-  static constexpr int ST = DP == 128 ? 3 : 6;                                     // blocks in flight: 192 KB
+  static constexpr int KB = CfwParams<DP>::KB, NC = DP / 64, CHUNK = KB * 128, TILE = NC * CHUNK;      // K or V of a block
+  static constexpr int ST = 3;                                                     // blocks in flight: 192 KB
+  static constexpr int KEYS = KB / CFW_WARPS;                                      // of a warp
   static constexpr int JOIN = CFW_WARPS * 8 * DP * 4;                              // eight rows of every warp's O
   static constexpr int SMEM = 2 * ST * TILE + JOIN + CFW_WARPS * CFW_ROWS * 8 + 256 + 64;
 };
@@ -77,7 +82,7 @@ __device__ __forceinline__ void cfw_sync() { asm volatile("bar.sync 1, %0;" ::"n
 
 template <class T, int DP>
 __global__ void __launch_bounds__(CFW_THREADS, 1)
-causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CfwParams p) {
+causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CfwParams<DP> p) {
   using Sh = CfwShape<DP>;
   constexpr int ST = Sh::ST;
   extern __shared__ __align__(1024) uint8_t cfw_smem[];
@@ -118,7 +123,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     p.desc[2 * blockIdx.x + threadIdx.x] = d;
   }
-  CausalWalk<CfwParams> walk;
+  CausalWalk<CfwParams<DP>> walk;
   walk.start(p, from, units);
   CausalSeg s;
   int stage = 0, use = 0;
@@ -129,7 +134,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const CUtensorMap* tm = is_k ? &tmK : &tmV;
     uint64_t* full = is_k ? k_full : v_full;
     uint8_t* ring = is_k ? sK : sV;
-    const int per = CFW_KB / p.box_rows;                  // boxes of 64 columns in a block
+    const int per = Sh::KB / p.box_rows;                  // boxes of 64 columns in a block
     const int chunk = lane / per, box = lane - chunk * per;
     int bad = 0;
 #pragma unroll 1
@@ -138,13 +143,13 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const int* ids = p.c.table + s.r * p.c.table_stride;
       // the page of this lane's box, looked up a block ahead
       auto page_of = [&](int j) {
-        const int row = j * CFW_KB + box * p.box_rows;
+        const int row = j * Sh::KB + box * p.box_rows;
         return chunk < Sh::NC && j < s.j1 && row < ctx ? ids[row / p.c.page] : 0;
       };
       int id = page_of(s.j0);
 #pragma unroll 1
       for (int j = s.j0; j < s.j1; ++j) {
-        const int row = j * CFW_KB + box * p.box_rows;
+        const int row = j * Sh::KB + box * p.box_rows;
         const bool mine = chunk < Sh::NC && row < ctx;
         const int ahead = page_of(j + 1);
         if (use > 0) ptx::mbar_wait_warp(&freed[stage], (use - 1) & 1, dead);
@@ -165,12 +170,12 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     if (bad && p.c.status) atomicOr(p.c.status, bad);
   } else {
-    // ---- consumers: keys 16 warp .. 16 warp + 15 of every block
+    // ---- consumers: an eighth of the keys of every block, 16 at a time
     const float c = p.scale_log2e;
     const int r0 = lane >> 2, col = (lane & 3) * 2;       // rows r0 and r0 + 8, columns col, col + 1 of each 8
     // places of ldmatrix: of K the keys are matrix columns, of V (transposed) matrix rows
-    const int k_key = warp * 16 + (lane & 7) + ((lane >> 4) << 3), k_unit = (lane >> 3) & 1;
-    const int v_key = warp * 16 + (lane & 15), v_unit = lane >> 4;
+    const int k_key = warp * Sh::KEYS + (lane & 7) + ((lane >> 4) << 3), k_unit = (lane >> 3) & 1;
+    const int v_key = warp * Sh::KEYS + (lane & 15), v_unit = lane >> 4;
     const uint32_t k_base = ptx::smem_u32(sK) + k_key * 128, v_base = ptx::smem_u32(sV) + v_key * 128;
 #pragma unroll 1
     while (walk.next(p, s)) {
@@ -199,11 +204,16 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll 1
       for (int j = s.j0; j < s.j1; ++j) {
-        const int key0 = j * CFW_KB + warp * 16;
         ptx::mbar_wait_warp(&k_full[stage], use & 1, dead);
-        if (key0 < ctx) {
+#pragma unroll
+        for (int kg = 0; kg < Sh::KEYS; kg += 16) {
+          const int key0 = j * Sh::KB + warp * Sh::KEYS + kg;
+          if (key0 >= ctx) {
+            if (kg == 0) ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
+            break;
+          }
           float sc[2][4] = {};
-          const uint32_t ka = k_base + stage * Sh::TILE;
+          const uint32_t ka = k_base + stage * Sh::TILE + kg * 128;
 #pragma unroll
           for (int kk = 0; kk < DP / 16; ++kk) {
             if (kk < p.ksteps) {
@@ -247,12 +257,12 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
               pa[h + 2 * t] = CfwType<T>::pack(x, y);
             }
           }
-          ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
+          if (kg == 0) ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
           if (key0 + 16 > ctx) {
             // values behind the request's last key: zeros
             const int key = lane >> 1;
             if (key0 + key >= ctx) {
-              uint4* v = reinterpret_cast<uint4*>(sV + stage * Sh::TILE + (warp * 16 + key) * 128) + (lane & 1) * 4;
+              uint4* v = reinterpret_cast<uint4*>(sV + stage * Sh::TILE + (warp * Sh::KEYS + kg + key) * 128) + (lane & 1) * 4;
 #pragma unroll
               for (int h = 0; h < Sh::NC; ++h)
 #pragma unroll
@@ -261,7 +271,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
             }
             __syncwarp();
           }
-          const uint32_t va = v_base + stage * Sh::TILE;
+          const uint32_t va = v_base + stage * Sh::TILE + kg * 128;
 #pragma unroll
           for (int dt = 0; dt < DP / 16; ++dt) {
             if (dt < p.ksteps) {
@@ -271,8 +281,6 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
               CfwType<T>::mma(o[2 * dt + 1], pa, b[2], b[3]);
             }
           }
-        } else {
-          ptx::mbar_wait_warp(&v_full[stage], use & 1, dead);
         }
         __syncwarp();
         ptx::mbar_arrive_warp(&freed[stage]);
@@ -345,7 +353,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
 // Puts the parts of a cut item together: CTA c the item that CTA c of the attention began and left unfinished, if any; a warp per row,
 // parts in their order.
 template <class T, int DP>
-__global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_constant__ CfwParams p) {
+__global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_constant__ CfwParams<DP> p) {
   const int c = blockIdx.x, r = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::pdl_launch();
   ptx::pdl_wait();

@@ -2,6 +2,7 @@
 // causal attention over packed prompts and over the cache.  Checks of arguments, choice of kernel, launches.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -124,6 +125,7 @@ void check_attention(Check& c, const AttnCall& a) {
   c.need(a.n_heads >= 1 && a.n_kv >= 1 && a.n_heads <= 4096 && a.n_heads % a.n_kv == 0, SOD2_E_BAD_DIM, "the heads must be a multiple of the key heads");
   c.need(a.dim >= 1 && a.dim <= 256, SOD2_E_BAD_DIM, "head size must be 1..256");
   c.need(a.n_req >= 0 && a.n_tokens >= 0 && a.n_tokens <= kMaxRows && a.n_req <= kMaxRows, SOD2_E_BAD_DIM, "number of requests or tokens");
+  c.need(c.status != SOD2_OK || a.n_tokens * a.n_heads < int64_t(1) << 33, SOD2_E_BAD_DIM, "tokens x heads");      // a grid of the simple form
   c.need(std::isfinite(a.scale) && a.scale > 0, SOD2_E_INVALID_ARG, "scale must be positive and finite");
   if (c.status != SOD2_OK || a.n_req == 0 || a.n_tokens == 0) return;
   check_rows(c, a.q, esz, "null queries");
@@ -159,19 +161,40 @@ void set_parts(P& a, const Parts& at, void* ws) {
   a.part_o = reinterpret_cast<float*>(w + at.o);
 }
 
+// More than 48 KB of shared memory have to be allowed, for each kernel on each device; `done` has a bit per device.
+template <class K>
+cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 template <class T, int DP>
 cudaError_t launch_tiles(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& a, cudaStream_t st) {
-  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_tcgen05<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CtcShape<DP>::SMEM);
-  if (once != cudaSuccess) return once;
-  const cudaError_t e = launch(k::causal_attention_tcgen05<T, DP>, dim3(k::CTC_GRID), k::CTC_THREADS, k::CtcShape<DP>::SMEM, st, q, kk, v, a);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(k::causal_attention_tcgen05<T, DP>, k::CtcShape<DP>::SMEM, done);
+  if (e == cudaSuccess) e = launch(k::causal_attention_tcgen05<T, DP>, dim3(k::CTC_GRID), k::CTC_THREADS, k::CtcShape<DP>::SMEM, st, q, kk, v, a);
   return e != cudaSuccess || !a.cut ? e : launch(k::causal_join<T, DP>, dim3(k::CTC_GRID, 2), DP * 8, 0, st, a);
 }
 
 template <class T, int DP>
-cudaError_t launch_few(const CUtensorMap& kk, const CUtensorMap& v, const k::CfwParams& a, cudaStream_t st) {
-  static const cudaError_t once = cudaFuncSetAttribute(k::causal_attention_few<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, k::CfwShape<DP>::SMEM);
-  if (once != cudaSuccess) return once;
-  const cudaError_t e = launch(k::causal_attention_few<T, DP>, dim3(k::CFW_GRID), k::CFW_THREADS, k::CfwShape<DP>::SMEM, st, kk, v, a);
+cudaError_t launch_few(const CUtensorMap& kk, const CUtensorMap& v, const k::CausalParams& p, int few, bool all, int ksteps, int box_rows, int64_t max_keys, void* ws, cudaStream_t st) {
+  using P = k::CfwParams<DP>;
+  P a{};
+  a.c = p;
+  a.scale_log2e = p.scale * 1.4426950408889634f;
+  a.G = p.H / p.HK; a.ksteps = ksteps; a.box_rows = box_rows;
+  a.cut = max_keys > (P::WHOLE - 1) * P::KB;
+  a.most = all ? 0x7fffffff : few;
+  set_parts(a, few_parts(DP), ws);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(k::causal_attention_few<T, DP>, k::CfwShape<DP>::SMEM, done);
+  if (e == cudaSuccess) e = launch(k::causal_attention_few<T, DP>, dim3(k::CFW_GRID), k::CFW_THREADS, k::CfwShape<DP>::SMEM, st, kk, v, a);
   return e != cudaSuccess || !a.cut ? e : launch(k::causal_few_join<T, DP>, dim3(k::CFW_GRID), k::CFW_ROWS * 32, 0, st, a);
 }
 
@@ -204,15 +227,8 @@ bool tensor_core_attention(const k::CausalParams& p, int dtype, int64_t max_new,
   }
   e = cudaSuccess;
   if (few > 0) {
-    k::CfwParams b{};
-    b.c = p;
-    b.scale_log2e = p.scale * 1.4426950408889634f;
-    b.G = G; b.ksteps = ksteps; b.box_rows = box_rows;
-    b.cut = max_keys > (k::CfwParams::WHOLE - 1) * k::CFW_KB;
-    b.most = all_few ? 0x7fffffff : few;
-    set_parts(b, few_parts(dp), ws);
-    if (f16) e = dp == 64 ? launch_few<__half, 64>(mk, mv, b, st) : launch_few<__half, 128>(mk, mv, b, st);
-    else e = dp == 64 ? launch_few<__nv_bfloat16, 64>(mk, mv, b, st) : launch_few<__nv_bfloat16, 128>(mk, mv, b, st);
+    auto* run = f16 ? (dp == 64 ? launch_few<__half, 64> : launch_few<__half, 128>) : (dp == 64 ? launch_few<__nv_bfloat16, 64> : launch_few<__nv_bfloat16, 128>);
+    e = run(mk, mv, p, few, all_few, ksteps, box_rows, max_keys, ws, st);
   }
   if (!all_few && e == cudaSuccess) {
     a.c = p;

@@ -322,6 +322,145 @@ def test_paged_attention_behind_four_billion_elements():
         close(out, want, R.attention_tolerance("bf16", want, mass))
 
 
+# ------------------------------------------------------------------------------------------------ both forms of the attention, further
+def prompt_case(dtype, lens, H, kv, dim, seed=0, scale=None, change=None, packed=True):
+    scale = 1 / math.sqrt(dim) if scale is None else scale
+    cu, T = cumulative(lens), sum(lens)
+    x = randn(T, H + 2 * kv, dim, seed=seed, dtype=dtype)
+    x[:, :H] *= 2
+    if change:
+        change(x, cu)
+    q, k, v = x[:, :H], x[:, H:H + kv], x[:, H + kv:]
+    if not packed:
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    out, status = torch.full((T, H, dim), 5.0, dtype=x.dtype, device="cuda"), ints([0])
+    R.prompt(dtype, q, k, v, out, ints(cu), scale, status)
+    assert int(status) == 0
+    return cu, q, k, v, out, scale
+
+
+def check_prompt(dtype, lens, *args, **kw):
+    cu, q, k, v, out, scale = prompt_case(dtype, lens, *args, **kw)
+    for a, b in zip(cu, cu[1:]):
+        want, mass = R.attend(q[a:b], k[a:b], v[a:b], b - a, scale)
+        close(out[a:b], want, R.attention_tolerance(dtype, want, mass))
+
+
+def test_more_requests_than_a_cta_has_threads():
+    rng = random.Random(5)
+    check_prompt("bf16", [rng.randint(0, 5) for _ in range(900)], 4, 2, 64)
+    check_prompt("bf16", [rng.randint(0, 3) for _ in range(400)] + [1500] + [2] * 300, 4, 2, 128)
+    check_paged("f16", [1] * 700, [rng.randint(1, 90) for _ in range(700)], 4, 2, 64, 16, max_new=1)
+    check_paged("bf16", [rng.choice([0, 1, 1, 30]) for _ in range(450)], [rng.randint(30, 60) for _ in range(450)], 4, 2, 128, 32)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_of_random_shapes(seed):
+    rng = random.Random(100 + seed)
+    dtype, kv = rng.choice(["bf16", "f16"]), rng.choice([1, 2, 3])
+    H, dim = kv * rng.choice([1, 2, 3, 4, 7, 8, 16, 32]), rng.choice([8, 24, 40, 64, 72, 80, 96, 104, 128])
+    n = rng.randint(1, 6)
+    most = rng.choice([5, 60, 700])
+    lens = [rng.choice([0, 1, rng.randint(1, most), most]) for _ in range(n)] + [1]
+    check_prompt(dtype, lens, H, kv, dim, seed, packed=rng.random() < 0.5)
+    past = [rng.choice([0, rng.randint(0, 100), rng.randint(0, 3000)]) for _ in lens]
+    check_paged(dtype, lens, [p + v for p, v in zip(past, lens)], H, kv, dim, rng.choice([8, 16, 40, 64, 128, 384]),
+                rng.choice(["page, token, head", "page, head, token"]), max_new=rng.choice([0, most]))
+
+
+def test_one_token_alone():
+    check_prompt("bf16", [1], 4, 2, 64)
+    check_paged("bf16", [1], [1], 32, 1, 64, 16, pad=0)
+    check_paged("bf16", [1], [900], 20, 1, 128, 16, pad=0)             # more heads a key head than rows of the few-row form
+
+
+def test_references_that_rise_with_every_block():
+    # keys that grow: the largest score is always in the last block, by far more than the reference may lag behind
+    def grow(x, cu):
+        T = x.shape[0]
+        x[:, 4:6] = x[:, :1] * torch.linspace(0.05, 6, T, device="cuda")[:, None, None].to(x.dtype)
+    for dim in (64, 128):
+        check_prompt("bf16", [1100], 4, 2, dim, change=grow, scale=0.02)
+    q_dir = randn(1, 4, 128, seed=3)
+    for new in (1, 40):
+        ctx, page = 1500, 16
+        kc, vc, table = make_cache([ctx], page, 2, 128, "f16")
+        ramp = torch.linspace(0, 4, ctx, device="cuda")
+        for j, p in enumerate(table[0][:-(-ctx // page)]):
+            m = min(page, ctx - j * page)
+            kc[p, :m] = (q_dir[0, ::2][None] * ramp[j * page:j * page + m, None, None]).to(kc.dtype)
+        q, out = q_dir.to(kc.dtype).expand(new, 4, 128).contiguous(), torch.zeros(new, 4, 128, dtype=kc.dtype, device="cuda")
+        R.paged("f16", q, out, ints([0, new]), ints([ctx]), kc, vc, ints(table), 0.3, new)
+        want, mass = R.attend(q, R.gather_pages(kc, table[0], ctx), R.gather_pages(vc, table[0], ctx), ctx, 0.3)
+        close(out, want, R.attention_tolerance("f16", want, mass))
+
+
+@pytest.mark.parametrize("bad", [NAN, float("inf"), float("-inf")])
+def test_later_tokens_that_are_not_finite_do_not_reach_earlier_rows(bad):
+    # keys and values from a token on; whole items, cut ones, both forms
+    at = 700
+    for dim in (64, 128):
+        def spoil(x, cu):
+            x[at:, 4:] = bad
+        cu, q, k, v, out, scale = prompt_case("bf16", [1200], 4, 2, dim, change=spoil)
+        want, mass = R.attend(q[:at], k[:at], v[:at], at, scale)
+        close(out[:at], want, R.attention_tolerance("bf16", want, mass))
+        assert not out[at:].isfinite().all(-1).any()
+    H, kv, dim, page, new, ctx = 4, 2, 128, 16, 6, 3000
+    for n in (new, 60):
+        kc, vc, table = make_cache([ctx], page, kv, dim, "bf16")
+        first = ctx - n + n // 2                                       # the first token that is not finite
+        for t in range(first, ctx):
+            kc[table[0][t // page], t % page] = bad
+            vc[table[0][t // page], t % page] = bad
+        q = randn(n, H, dim)
+        out = torch.full_like(q, 5.0)
+        R.paged("bf16", q, out, ints([0, n]), ints([ctx]), kc, vc, ints(table), 0.1)
+        good = n // 2
+        want, mass = R.attend(q[:good], R.gather_pages(kc, table[0], ctx - n + good), R.gather_pages(vc, table[0], ctx - n + good), ctx - n + good, 0.1)
+        close(out[:good], want, R.attention_tolerance("bf16", want, mass))
+        assert not out[good:].isfinite().all(-1).any()
+
+
+def test_keys_that_all_heads_share():
+    # a broadcast key head: strides of zero, which no tensor map has
+    T, H, dim = 150, 4, 64
+    q, k1, v1 = randn(T, H, dim), randn(T, 1, dim, seed=1), randn(T, 1, dim, seed=2)
+    k, v = k1.expand(T, 2, dim), v1.expand(T, 2, dim)
+    out = torch.zeros_like(q)
+    R.prompt("bf16", q, k, v, out, ints([0, T]), 0.125)
+    want, mass = R.attend(q, k, v, T, 0.125)
+    close(out, want, R.attention_tolerance("bf16", want, mass))
+
+
+def test_two_captured_graphs_share_a_workspace():
+    H, kv, dim, page = 8, 2, 128, 16
+    ws, cases, graphs = R.Workspace(H, kv, dim), [], []
+    for new, ctx in (([1, 1], [2500, 900]), ([90, 300], [2000, 300])):
+        kc, vc, table = make_cache(ctx, page, kv, dim, "bf16", seed=sum(new))
+        q, cu, c, t = randn(sum(new), H, dim, seed=sum(ctx)), ints(cumulative(new)), ints(ctx), ints(table)
+        out = torch.zeros_like(q)
+        args = ("bf16", q, out, cu, c, kc, vc, t, 0.1, max(new), None, ws)
+        R.paged(*args)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            R.paged(*args)
+        cases.append((args, out.clone(), table))
+        graphs.append(g)
+    for _ in range(3):
+        for g, (args, first, table) in zip(graphs, cases):
+            args[2].fill_(7)
+            g.replay()
+            assert torch.equal(args[2], first)
+    # lengths are read when the graph runs
+    args, _, table = cases[0]
+    args[4].copy_(ints([700, 33]))
+    graphs[0].replay()
+    for r, m in enumerate((700, 33)):
+        want, mass = R.attend(args[1][r:r + 1], R.gather_pages(args[5], table[r], m), R.gather_pages(args[6], table[r], m), m, 0.1)
+        close(args[2][r:r + 1], want, R.attention_tolerance("bf16", want, mass))
+
+
 # ------------------------------------------------------------------------------------------------ together
 def serve(dtype, prompts, steps, H, kv, dim, page, qkv, captured=False):
     """Prompts in chunks, then single tokens, through all operators; per request the outputs of all its tokens.  qkv(r, a, b): the

@@ -57,7 +57,7 @@ PROMPT = [B.DTYPE_BF16, 2, 100, 4, 2, 64, ROWS, ROWS, ROWS, (2 * P, 256, 64), P,
 
 
 @pytest.mark.parametrize("changes,status", [
-    ({0: 7}, "INVALID_ARG"), ({1: -1}, "BAD_DIM"), ({2: -1}, "BAD_DIM"), ({2: 1 << 31}, "BAD_DIM"), ({3: 5}, "BAD_DIM"), ({3: 0}, "BAD_DIM"), ({4: 0}, "BAD_DIM"),
+    ({0: 7}, "INVALID_ARG"), ({1: -1}, "BAD_DIM"), ({2: -1}, "BAD_DIM"), ({2: 1 << 31}, "BAD_DIM"), ({2: 1 << 24, 3: 1024, 4: 8}, "BAD_DIM"), ({3: 5}, "BAD_DIM"), ({3: 0}, "BAD_DIM"), ({4: 0}, "BAD_DIM"),
     ({3: 8192}, "BAD_DIM"), ({5: 0}, "BAD_DIM"), ({5: 257}, "BAD_DIM"), ({6: None}, "INVALID_ARG"), ({7: None}, "INVALID_ARG"), ({8: (0, 1, 1)}, "INVALID_ARG"),
     ({9: None}, "INVALID_ARG"), ({9: ROWS}, "INVALID_ARG"), ({6: (P + 1, 256, 64)}, "MISALIGNED"), ({7: (P, -256, 64)}, "BAD_DIM"), ({10: None}, "INVALID_ARG"),
     ({11: 0.0}, "INVALID_ARG"), ({11: -1.0}, "INVALID_ARG"), ({11: float("inf")}, "INVALID_ARG"), ({11: float("nan")}, "INVALID_ARG")])
