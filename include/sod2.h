@@ -313,8 +313,14 @@ sod2_status sod2_rope_store(int dtype, int64_t n_tokens, int n_heads, int n_kv_h
                             const sod2_pages* k_cache, const sod2_pages* v_cache, int64_t n_pages, int page_size,
                             const int64_t* dev_slots, int32_t* dev_status, void* cuda_stream);
 
-/* Bytes of device workspace (256-byte aligned) for the two attention calls with these heads, whatever the number and lengths of
- * requests.  Calls that may overlap on the GPU need a workspace each; two captured graphs that never overlap may share one. */
+/* Bytes of device workspace for the two attention calls with these heads, whatever the number and lengths of requests (42 MB at
+ * head sizes 72 to 128); the workspace must be 256-byte aligned, needs no initial contents and holds nothing between calls.  Calls that may
+ * overlap on the GPU need a workspace each; two captured graphs that never overlap may share one.
+ * Forms of the attention calls, all with 32-bit scores, maxima, sums and outputs that are rounded once:
+ *   bf16 and f16, head_dim a multiple of 8 up to 128, at most 128 heads a key head, 16-byte aligned addresses, strides that are multiples of
+ *     8 elements and not 0, page_size a multiple of 8: tensor cores fed by TMA.  The probabilities are rounded to the type of the values for their product.
+ *   everything else: a plain form, a warp per row and head, for correctness and not for speed.
+ * Keys and values that a row may not see do not reach it, whatever they hold, infinities and NaN included. */
 sod2_status sod2_attention_workspace_bytes(int n_heads, int n_kv_heads, int head_dim, size_t* bytes);
 
 /* Causal attention over packed prompts with grouped heads: request r has the rows dev_cu_tokens[r] .. dev_cu_tokens[r + 1] - 1 of q,

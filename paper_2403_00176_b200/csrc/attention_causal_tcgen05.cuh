@@ -42,15 +42,15 @@ namespace sod2 {
 namespace k {
 
 constexpr int CTC_THREADS = 384;
+constexpr int CTC_REGS = 168, CTC_REGS_SOFTMAX = 208, CTC_REGS_OTHERS = 88;      // a thread: at the start, and shared out
+static_assert(2 * CTC_REGS_SOFTMAX + CTC_REGS_OTHERS == 3 * CTC_REGS, "setmaxnreg waits for registers that the CTA does not have");
 constexpr int CTC_GRID = 148;              // CTAs of the division: one per SM
 constexpr int CTC_KB = 128;                // keys per block
 constexpr int CTC_CHUNK = 128 * 128;       // bytes of 128 rows x 64 elements
 constexpr int CTC_START = 3;               // weight of an item's start and end, in blocks (1: 908, 2: 1015, 3: 1034 TFLOP/s at 8192 tokens; the first
                                            // items of a head are the shortest, and their CTAs end last where it is too low)
-#ifndef CTC_WHOLE_VALUE
-#define CTC_WHOLE_VALUE 8
-#endif
-constexpr int CTC_WHOLE = CTC_WHOLE_VALUE;               // blocks: shorter items are not cut
+constexpr int CTC_WHOLE = 8;               // blocks: shorter items are not cut (4, 8, 12, 24: 8 prompts of 16 to 512 tokens, 12 heads of 64 over 4, 22.3, 17.9,
+                                           // 18.0, 16.9 us; 8192 tokens, 12 heads of 64, 182.5, 181.3, 181.8, 188.2 us)
 constexpr int CTC_SNAP = 2;                // blocks: cuts closer than this to an item's ends move there
 
 struct CtcParams {
@@ -174,7 +174,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   if (warp == 10) { ptx::tmem_alloc(tmem_slot, 512); ptx::tmem_relinquish(); }
   ptx::pdl_wait();
   causal_divide(p, weight, spot);
-  ptx::fence_proxy_async();           // the plan's scratch becomes the load ring
+  ptx::fence_proxy_async();           // the division's scratch becomes the load ring
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
@@ -205,9 +205,9 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     return e > g.j0 ? e - g.j0 : 0;
   };
 
-  // the 168 registers a thread that the CTA starts with (3 x 168 = 504 for the three warps of a quarter) are shared out: 2 x 208 + 88
+  // The registers that the CTA starts with are shared out anew (the host checks that it starts with so many).  Softmax threads hold 128 scores.
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CTC_REGS_OTHERS));
     if (warp < 10) {
       // ---- TMA producers: warp 8 Q and the K tiles, warp 9 the V tiles
       const bool is_k = warp == 8;
@@ -389,7 +389,7 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     }
   } else {
     // ---- softmax warps: tile t = warp / 4, a thread per row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CTC_REGS_SOFTMAX));
     const int t = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + Sh::TM_S + t * 128, tO = tmem + lane_base + Sh::TM_O + t * DP;

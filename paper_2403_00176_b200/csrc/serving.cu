@@ -161,15 +161,21 @@ void set_parts(P& a, const Parts& at, void* ws) {
   a.part_o = reinterpret_cast<float*>(w + at.o);
 }
 
-// More than 48 KB of shared memory have to be allowed, for each kernel on each device; `done` has a bit per device.
+// More than 48 KB of shared memory have to be allowed, for each kernel on each device; `done` has a bit per device.  regs: the registers a
+// thread that the kernel has to start with (0: any), for one that shares them out itself.
 template <class K>
-cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& done) {
+cudaError_t allow_smem(K* kernel, int bytes, int regs, std::atomic<uint64_t>& done) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
   if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && regs) {
+    cudaFuncAttributes at{};
+    e = cudaFuncGetAttributes(&at, kernel);
+    if (e == cudaSuccess && at.numRegs != regs) e = cudaErrorInvalidKernelImage;
+  }
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
   return e;
 }
@@ -177,7 +183,7 @@ cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& done) {
 template <class T, int DP>
 cudaError_t launch_tiles(const CUtensorMap& q, const CUtensorMap& kk, const CUtensorMap& v, const k::CtcParams& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem(k::causal_attention_tcgen05<T, DP>, k::CtcShape<DP>::SMEM, done);
+  cudaError_t e = allow_smem(k::causal_attention_tcgen05<T, DP>, k::CtcShape<DP>::SMEM, k::CTC_REGS, done);
   if (e == cudaSuccess) e = launch(k::causal_attention_tcgen05<T, DP>, dim3(k::CTC_GRID), k::CTC_THREADS, k::CtcShape<DP>::SMEM, st, q, kk, v, a);
   return e != cudaSuccess || !a.cut ? e : launch(k::causal_join<T, DP>, dim3(k::CTC_GRID, 2), DP * 8, 0, st, a);
 }
@@ -193,7 +199,7 @@ cudaError_t launch_few(const CUtensorMap& kk, const CUtensorMap& v, const k::Cau
   a.most = all ? 0x7fffffff : few;
   set_parts(a, few_parts(DP), ws);
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem(k::causal_attention_few<T, DP>, k::CfwShape<DP>::SMEM, done);
+  cudaError_t e = allow_smem(k::causal_attention_few<T, DP>, k::CfwShape<DP>::SMEM, 0, done);
   if (e == cudaSuccess) e = launch(k::causal_attention_few<T, DP>, dim3(k::CFW_GRID), k::CFW_THREADS, k::CfwShape<DP>::SMEM, st, kk, v, a);
   return e != cudaSuccess || !a.cut ? e : launch(k::causal_few_join<T, DP>, dim3(k::CFW_GRID), k::CFW_ROWS * 32, 0, st, a);
 }
