@@ -47,21 +47,22 @@ struct CausalSeg { int r, head, idx, first, n, past, j0, j1; bool starts, ends; 
 template <class P>
 struct CausalWalk {
   long long left;
-  int r, head, idx, off;
+  int r, head, idx, off, items;           // items: of the request and a head
   CausalReq q;
   __device__ __forceinline__ void start(const P& p, const CausalSpot& a, long long units) {
-    left = units; r = a.r; head = a.head; idx = a.idx; off = a.off;
+    left = units; r = a.r; head = a.head; idx = a.idx; off = a.off; items = 0;
     q.n = 0;
-    if (left > 0) q = causal_request(p, r);
+    if (left > 0) { q = causal_request(p, r); items = p.items(q); }
   }
   __device__ __forceinline__ bool next(const P& p, CausalSeg& s) {
     if (left <= 0) return false;
-    while (idx >= p.items(q)) {
+    while (idx >= items) {
       idx = 0;
       if (q.n > 0 && ++head < p.c.HK) continue;
       head = 0;
       if (++r >= p.c.n_req) { left = 0; return false; }
       q = causal_request(p, r);
+      items = p.items(q);
     }
     const int blocks = causal_item_blocks(p, q, idx), w = blocks + P::START;
     const int end = left < w - off ? off + static_cast<int>(left) : w;

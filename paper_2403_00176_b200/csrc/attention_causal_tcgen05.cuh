@@ -494,31 +494,34 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         const int h = s.head * p.G + rg;
         const long long orow = s.first + t0 + rt;
         T* o = static_cast<T*>(p.c.o) + orow * p.c.o_ts + h * p.c.o_hs;
-        bool odd = false;                                   // something not finite
+        // Two columns an instruction, and a product with zero for each to tell what is not finite: two warps share a scheduler here, and
+        // instructions are what it takes (a comparison for each column and 16 columns at a time: 1% more time at 31,696 tokens)
+        float2 odd2 = make_float2(0.f, 0.f);
+        const float2 inv2 = make_float2(inv, inv);
 #pragma unroll 1
-        for (int d = 0; d < p.c.D; d += 16) {
-          uint32_t r[16];
+        for (int d = 0; d < p.c.D; d += 32) {               // (columns behind the head size hold anything)
+          uint32_t r[32];
           if (mine > 0 && live) {
-            ptx::tmem_ld8(tO + d, r);
-            ptx::tmem_ld8(tO + d + 8, r + 8);
+            ptx::tmem_ld32(tO + d, r);
             ptx::tmem_ld_wait();
           } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) r[e] = 0;
+            for (int e = 0; e < 32; ++e) r[e] = 0;
           }
-          uint4 v[2];
-          uint32_t* w = reinterpret_cast<uint32_t*>(v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = __uint_as_float(r[2 * e]) * inv, y = __uint_as_float(r[2 * e + 1]) * inv;
-            odd |= !(fabsf(x) < INFINITY) || !(fabsf(y) < INFINITY);
-            w[e] = CtcType<T>::pack(x, y);
-          }
-          if (valid) {
-            *reinterpret_cast<uint4*>(o + d) = v[0];
-            if (d + 8 < p.c.D) *reinterpret_cast<uint4*>(o + d + 8) = v[1];
-          }
+          for (int g = 0; g < 4; ++g)
+            if (d + g * 8 < p.c.D) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float2 x = ptx::mul_x2(make_float2(__uint_as_float(r[g * 8 + 2 * e]), __uint_as_float(r[g * 8 + 2 * e + 1])), inv2);
+                odd2 = ptx::fma_x2(x, make_float2(0.f, 0.f), odd2);
+                w[e] = CtcType<T>::pack(x.x, x.y);
+              }
+              if (valid) *reinterpret_cast<uint4*>(o + d + g * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
+        const bool odd = !(odd2.x + odd2.y == 0.f);         // something not finite
         unsigned redo = __ballot_sync(0xffffffffu, valid && odd);
         __syncwarp();                                       // the rows written above are written again by the whole warp
         while (redo) {                                      // rare: see the top of the file
@@ -533,14 +536,14 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (live) {
 #pragma unroll 1
           for (int d = 0; d < p.n_pv; d += 16) {
-            uint32_t r[16];
+            uint32_t r[16] = {};
             if (mine > 0) {
               ptx::tmem_ld8(tO + d, r);
               ptx::tmem_ld8(tO + d + 8, r + 8);
               ptx::tmem_ld_wait();
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) po[(d + e) * 128] = mine > 0 ? __uint_as_float(r[e]) : 0.f;
+            for (int e = 0; e < 16; ++e) po[(d + e) * 128] = __uint_as_float(r[e]);
           }
           p.part_ml[tile * 128 + row] = make_float2(mine > 0 && m != -INFINITY ? m * c : -INFINITY, mine > 0 ? lsum : 0.f);
         }
