@@ -27,7 +27,13 @@
 //
 // Other shapes that were built and measured (8192 tokens, 32 heads of 128 over 8; this one 1034 TFLOP/s): one tile per CTA with two
 // warpgroups taking blocks in turn, S and P double buffered (974), the same with three warpgroups and P over S (908).  They
-// keep the tensor pipe and the exponentials apart better, but take in twice the keys and values per row.
+// keep the tensor pipe and the exponentials apart better, but take in twice the keys and values per row.  Two threads a row, 16 softmax
+// warps that exchange maxima (31,696 tokens in five prompts: 2693 us against 2626); S in two halves, the one that P does not lie
+// over issued ahead of the product's commit (2807).
+//
+// What bounds it: a block of both tiles takes 3600 cycles where tensor pipe and exponentials need 2048 each.  A tile's chain is 100 to load S,
+// 350 for the maximum, 1640 for P, then 256 of the product's second half, 512 of S and twice 370 from commit to wait.  The
+// chain alone is not it: without the wait for the product a block takes 2% less; without exponentials still 3000.
 //
 // Warps: 0..3 softmax of tile A, 4..7 of tile B, 8 loads Q and K, 9 loads V, 10 issues the MMAs.  A box of the cache is the part of a
 // page that lies in a block; lanes issue boxes side by side: a lane on its own sustains one per 440 cycles (16 rows: 1.3 TB/s
