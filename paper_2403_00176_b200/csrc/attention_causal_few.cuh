@@ -314,8 +314,8 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
           for (int w = 0; w < CFW_WARPS; ++w) {
             const float2 ml = ml_s[w * CFW_ROWS + r];
             const float f = ml.x == -INFINITY ? 0.f : cfw_ex2((ml.x - top) * c);
-            if (ml.x != -INFINITY) {                        // (a warp whose keys the row did not see; NaN goes on)
-              sum = fmaf(f, ml.y, sum);
+            sum = fmaf(f, ml.y, sum);                       // (no maximum: no key that the row sees, 0, or only scores that are no numbers, NaN)
+            if (ml.x != -INFINITY) {
               const float* src = o_s + (w * 8 + warp) * DP + ((lane * PER) ^ ((warp & 3) << 3));
 #pragma unroll
               for (int e = 0; e < PER; ++e) acc[e] = fmaf(f, src[e], acc[e]);
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(CFW_ROWS * 32) causal_few_join(const __grid_co
   for (int i0 = c; i0 <= last; i0 += 32) {
     const float2 ml = part(i0 + lane);
     const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
-    l += ml.x == -INFINITY ? 0.f : w * ml.y;
+    l = fmaf(w, ml.y, l);
     const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);
     // eight parts' rows on their way at a time
 #pragma unroll 1

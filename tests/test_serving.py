@@ -422,6 +422,27 @@ def test_later_tokens_that_are_not_finite_do_not_reach_earlier_rows(bad):
         assert not out[good:].isfinite().all(-1).any()
 
 
+@pytest.mark.parametrize("ctx", [1, 17, 1040, 5000])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_visible_key_that_is_not_a_number_makes_the_row_so(ctx, dim):
+    kc, vc, table = make_cache([ctx, ctx], 16, 1, dim, "bf16", fill=0.0)
+    kc[table[1][(ctx - 1) // 16], (ctx - 1) % 16] = NAN         # the last key of the second request, alone among its warp's 16 for most ctx
+    q, out = randn(2, 2, dim, seed=3), torch.zeros(2, 2, dim, dtype=torch.bfloat16, device="cuda")
+    for max_new in (1, 0):
+        R.paged("bf16", q, out, ints([0, 1, 2]), ints([ctx, ctx]), kc, vc, ints(table), dim ** -0.5, max_new=max_new)
+        assert out[0].isfinite().all() and out[1].isnan().all()
+
+
+@pytest.mark.parametrize("heads", range(1, 17))
+def test_keys_that_are_not_numbers_in_every_part_of_a_cut_row(heads):
+    # the last 256 keys: the diagonal ones lie in a block of which the row sees nothing else, for some numbers of heads in a part of its own
+    q, k, v = (randn(2048, heads, 64, seed=s) for s in range(3))
+    k[1792:] = NAN
+    out = torch.zeros_like(q)
+    R.prompt("bf16", q, k, v, out, ints([0, 2048]), 0.125)
+    assert out[:1792].isfinite().all() and out[1792:].isnan().all()
+
+
 def test_keys_that_all_heads_share():
     # a broadcast key head: strides of zero, which no tensor map has
     T, H, dim = 150, 4, 64
