@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <string>
 #include <type_traits>
 
@@ -58,6 +59,12 @@ void on_current_device(Check& c, const void* p) {
 
 int elem_size(int dtype) { return dtype == SOD2_DTYPE_F32 ? 4 : dtype == SOD2_DTYPE_BF16 || dtype == SOD2_DTYPE_F16 ? 2 : 0; }
 bool on(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// Arrays of 32- and 64-bit integers (null is aligned).
+void check_ints(Check& c, std::initializer_list<const void*> i32, const void* i64 = nullptr) {
+  for (const void* p : i32) c.need(on(p, 4), SOD2_E_MISALIGNED, "an array of integers is not aligned to its elements");
+  c.need(on(i64, 8), SOD2_E_MISALIGNED, "an array of integers is not aligned to its elements");
+}
 
 void check_rows(Check& c, const sod2_rows* r, int esz, const char* what) {
   c.need(r && r->data, SOD2_E_INVALID_ARG, what);
@@ -289,6 +296,7 @@ extern "C" sod2_status sod2_page_tables(int n_requests, int64_t max_tokens, int 
     c.need(n_requests == 0 || table_width == 0 || dev_table, SOD2_E_INVALID_ARG, "null table");
     // CTAs read the lengths and the head while others write their outputs
     c.need(dev_free_head_out != dev_free_head && (!dev_ctx || (dev_ctx != dev_past && dev_ctx != dev_new)), SOD2_E_INVALID_ARG, "an output is an input");
+    check_ints(c, {dev_past, dev_new, dev_free_pages, dev_free_head, dev_table, dev_cu_tokens, dev_ctx, dev_positions, dev_free_head_out, dev_status}, dev_slots);
     on_current_device(c, dev_cu_tokens);
     if (c.status != SOD2_OK) return c.fail();
     k::PageTableParams p{};
@@ -337,6 +345,7 @@ extern "C" sod2_status sod2_rope_store(int dtype, int64_t n_tokens, int n_heads,
       c.need(page_size >= 1 && n_pages >= 0 && n_pages <= INT64_MAX / page_size, SOD2_E_BAD_DIM, "pages of the cache");
     }
     c.need(dev_positions != nullptr, SOD2_E_INVALID_ARG, "null positions");
+    check_ints(c, {dev_positions, dev_status}, dev_slots);
     if (c.status == SOD2_OK) for (int j = 0; j < n_pairs; ++j) c.need(std::isfinite(freq[j]), SOD2_E_INVALID_ARG, "a frequency is not finite");
     if (c.status == SOD2_OK && n_tokens == 0) return SOD2_OK;
     if (c.status == SOD2_OK) on_current_device(c, q ? q_out->data : k->data);
@@ -391,6 +400,7 @@ extern "C" sod2_status sod2_attention_prompt(int dtype, int n_requests, int64_t 
     if (c.status == SOD2_OK && (n_requests == 0 || n_tokens == 0)) return SOD2_OK;
     check_rows(c, k, elem_size(dtype), "null keys");
     check_rows(c, v, elem_size(dtype), "null values");
+    check_ints(c, {dev_cu_tokens, dev_status});
     c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k->data && out->data != v->data), SOD2_E_INVALID_ARG, "the output is an input");
     check_workspace(c, head_dim, dev_workspace, workspace_bytes);
     if (c.status == SOD2_OK) on_current_device(c, out->data);
@@ -421,6 +431,7 @@ extern "C" sod2_status sod2_attention_paged(int dtype, int n_requests, int64_t n
     check_pages(c, v_cache, elem_size(dtype), "null value cache");
     c.need(dev_ctx != nullptr, SOD2_E_INVALID_ARG, "null contexts");
     c.need(table_width == 0 || dev_table, SOD2_E_INVALID_ARG, "null table");
+    check_ints(c, {dev_cu_tokens, dev_ctx, dev_table, dev_status});
     c.need(c.status != SOD2_OK || (out->data != q->data && out->data != k_cache->data && out->data != v_cache->data), SOD2_E_INVALID_ARG, "the output is an input");
     check_workspace(c, head_dim, dev_workspace, workspace_bytes);
     if (c.status == SOD2_OK) on_current_device(c, out->data);

@@ -77,6 +77,14 @@ def test_paged_attention_refuses(changes, status):
     refused(status, B.sod2_attention_paged, *with_changes(PAGED, changes))
 
 
+@pytest.mark.parametrize("fn,base,which", [(B.sod2_page_tables, TABLES, {3: 2, 4: 1, 5: 2, 7: 2, 8: 2, 11: 2, 12: 1, 13: 4, 14: 2, 15: 2, 16: 2}),
+                                           (B.sod2_rope_store, ROPE, {6: 2, 17: 4, 18: 1}), (B.sod2_attention_prompt, PROMPT, {10: 2, 14: 2}),
+                                           (B.sod2_attention_paged, PAGED, {9: 2, 10: 1, 15: 2, 21: 2})])
+def test_integers_off_their_alignment_are_refused(fn, base, which):
+    for i, off in which.items():
+        refused("MISALIGNED", fn, *with_changes(base, {i: 2 * P + off}))
+
+
 def test_workspace_refuses():
     for heads in ((0, 1, 64), (4, 0, 64), (4, 3, 64), (4, 2, 0), (4, 2, 257)):
         refused("BAD_DIM", B.sod2_attention_workspace_bytes, *heads)
