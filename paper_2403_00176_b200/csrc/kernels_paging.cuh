@@ -143,6 +143,7 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables(const __grid_constant_
 
 // ---------------------------------------------------------------------------------------------- rotary positions
 constexpr int ROPE_MAX_PAIRS = 128;
+constexpr int ROPE_THREADS = 128, ROPE_CTAS = 8;      // (256 and 4: 40320 tokens, 24 heads of 64: 53.5 us against 50.7; 8192 tokens, 40 of 128, 45.0 against 42.1)
 struct RopeParams {
   const void* q; void* q_out; const void* k; void* k_out; const void* v;
   void* kc; void* vc; const long long* slots;
@@ -211,7 +212,7 @@ __device__ __forceinline__ void rope_turn(RopeVec<T, V>& x, RopeVec<T, V>& y, co
 // head (V pairs: 16 bytes of each side) and goes through heads `split` apart, two at a time.  Everything that does not hang on the angles is on its way
 // before they are worked out: a CTA's life is then one trip to memory and back and not four.
 template <class T, int V>
-__global__ void __launch_bounds__(256, 4) rope_store_rows(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(ROPE_THREADS, ROPE_CTAS) rope_store_rows(const __grid_constant__ RopeParams p) {
   extern __shared__ float2 turn_s[];       // [tile][pairs]
   using Vec = RopeVec<T, V>;
   constexpr int B = 2;
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(256, 4) rope_store_rows(const __grid_constant_
     const long long page = sl / p.page;
     return page * ps + (sl - page * p.page) * ts;
   };
-  const int vu = p.D / V, n_values = p.vc ? nt * p.HK * vu : 0, v_step = 256 * gridDim.y;
+  const int vu = p.D / V, n_values = p.vc ? nt * p.HK * vu : 0, v_step = ROPE_THREADS * gridDim.y;
   Vec val[2];
   long long to[2];
   auto load_values = [&](int i0) {
@@ -264,9 +265,9 @@ __global__ void __launch_bounds__(256, 4) rope_store_rows(const __grid_constant_
       }
     }
   };
-  const int v0 = blockIdx.y * 256 + threadIdx.x;
+  const int v0 = blockIdx.y * ROPE_THREADS + threadIdx.x;
   load_values(v0);
-  for (int i = threadIdx.x; i < n_angles; i += 256) {
+  for (int i = threadIdx.x; i < n_angles; i += ROPE_THREADS) {
     const int tt = i / p.pairs, j = i - tt * p.pairs;
     const int pos = i == static_cast<int>(threadIdx.x) ? pos0 : p.positions[p.axis[j] * p.pos_stride + t0 + tt];
     const double angle = p.turns[j] * static_cast<double>(pos);
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(256, 4) rope_store_rows(const __grid_constant_
   }
   // what lies behind the turned pairs, copied
   const int rot = 2 * p.pairs, cu = (p.D - rot) / V;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * HT * cu; i += 256 * gridDim.y) {
+  for (int i = blockIdx.y * ROPE_THREADS + threadIdx.x; i < nt * HT * cu; i += ROPE_THREADS * gridDim.y) {
     const int r = i / cu, u = rot + (i - r * cu) * V, tt = r / HT, h = r - tt * HT;
     const long long rr = t0 + tt;
     if (h < p.H) {

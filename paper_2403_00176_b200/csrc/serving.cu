@@ -103,19 +103,21 @@ cudaError_t launch(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cu
 
 template <class T, int V>
 cudaError_t launch_rope(const k::RopeParams& p, cudaStream_t st) {
-  const int heads = p.H + p.HK, places = 256 / (p.pairs / V);
+  const int heads = p.H + p.HK, places = k::ROPE_THREADS / (p.pairs / V);
   k::RopeParams q = p;
-  // Four heads a thread.  Fewer where that would leave SMs without a CTA: then fewer tokens a CTA, down to one, and heads shared out
-  // further, over CTAs too.
-  q.split = (heads + 3) / 4 < places ? (heads + 3) / 4 : places;
-  const int spread = (p.n_tokens + 2 * 148 - 1) / (2 * 148);
-  q.tile = places / q.split;
-  if (q.tile > spread) { q.tile = spread; q.split = places / q.tile < heads ? places / q.tile : heads; }
+  // About four heads a thread (six: 42.1 us as well at 8192 tokens of 40 heads, but 40.4 against 29.6 at 8191 of 32; eight: 46.3 and 34.7).  Fewer where
+  // that would leave SMs without a CTA: then fewer tokens a CTA, down to one, and heads shared out further, over CTAs too.
+  constexpr int want = 148 * 512 / k::ROPE_THREADS;
+  q.tile = (places * 4 + heads / 2) / heads;
+  q.tile = q.tile < 1 ? 1 : q.tile > places ? places : q.tile;
+  const int spread = (p.n_tokens + want - 1) / want;
+  if (q.tile > spread) q.tile = spread;
+  q.split = places / q.tile < heads ? places / q.tile : heads;
   const int gx = (p.n_tokens + q.tile - 1) / q.tile;
-  int gy = gx < 2 * 148 ? 2 * 148 / gx : 1;
+  int gy = gx < want ? want / gx : 1;
   const int most = (heads + q.split - 1) / q.split;
   gy = gy > most ? most : gy;
-  return launch(k::rope_store_rows<T, V>, dim3(gx, gy), 256, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st, q);
+  return launch(k::rope_store_rows<T, V>, dim3(gx, gy), k::ROPE_THREADS, static_cast<size_t>(q.tile) * p.pairs * sizeof(float2), st, q);
 }
 
 struct AttnCall {
