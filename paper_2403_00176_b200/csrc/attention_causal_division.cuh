@@ -207,5 +207,13 @@ __device__ __forceinline__ int causal_last_part(const int4* desc, int c, int gri
   return grid - 1;
 }
 
+// The end of a CTA in which a wait ran out: copies and MMAs that are still on their way get about a millisecond to land in shared memory
+// that is still the CTA's.
+__device__ __forceinline__ void causal_drain(const volatile int* dead) {
+  if (!*dead) return;
+  const long long until = clock64() + (1ll << 21);
+  while (clock64() < until) {}
+}
+
 }  // namespace k
 }  // namespace sod2

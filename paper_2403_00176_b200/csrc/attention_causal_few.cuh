@@ -347,6 +347,7 @@ causal_attention_few(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
   }
   __syncthreads();
+  causal_drain(dead);
   if (threadIdx.x == 0 && *dead && p.c.status) atomicOr(p.c.status, 1);
 }
 

@@ -279,6 +279,14 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           if (++stage == stages) { stage = 0; ++use; }
         }
       }
+      // the commits that nobody has waited for: their arrivals land before the CTA's shared memory is another's
+#pragma unroll 1
+      for (int b = 0; b < stages; ++b) {
+        const int uses = use + (b < stage);
+        if (uses > 0) ptx::mbar_wait_warp(&free_[b], (uses - 1) & 1, dead);
+      }
+      if (qn0 > 0) ptx::mbar_wait_warp(&q_free[0], (qn0 - 1) & 1, dead);
+      if (qn1 > 0) ptx::mbar_wait_warp(&q_free[1], (qn1 - 1) & 1, dead);
       if (bad && p.c.status) atomicOr(p.c.status, bad);
     } else if (warp == 10) {
       // ---- MMA issuer: the two tiles in turn, each time the product of a block and behind it S of the tile's next block, if need be of
@@ -560,6 +568,8 @@ causal_attention_tcgen05(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
   __syncwarp();
   ptx::tc_fence_before();
+  __syncthreads();
+  causal_drain(dead);
   __syncthreads();
   if (warp == 10) ptx::tmem_dealloc(tmem, 512);
   if (threadIdx.x == 0 && *dead && p.c.status) atomicOr(p.c.status, 1);
